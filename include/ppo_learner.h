@@ -240,6 +240,104 @@ int distill_update(ppo_ctx* ctx, const ppo_hparams* hp, ppo_mb_stats* host_stats
  * 0..count-1): action means to d_mu [count][A] fp32 and values to d_v [count] fp32 (may be NULL). */
 int ppo_forward(ppo_ctx* ctx, const int32_t* d_idx, int64_t count, float* d_mu, float* d_v);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Operators of a policy that answers in tokens (a categorical head over a vocabulary, sequences of uneven length).
+ *
+ * They need no context and allocate nothing: every array is the caller's, results included.  Work is enqueued on
+ * hip_stream (a hipStream_t, may be NULL) of the CURRENT device, where all arrays must lie; nothing synchronises, and
+ * every call may be recorded into a graph.  d_ws is scratch of at least the bytes that the *_ws_bytes function gives
+ * for the same sizes, 16-byte aligned; nothing is kept in it between calls, and two calls whose work may overlap in time
+ * need two of them (so do two captured graphs that may).  Errors are reported through ppo_last_error(NULL); arguments are
+ * checked before any HIP call.  Results are the same, bit for bit, every time.  An empty call (no rows, tokens or
+ * sequences) is allowed; the array pointers that it would read may then be NULL.
+ *
+ * `dtype` is the type of the large arrays: 0 fp32, 1 bf16, 2 fp16; everything else is fp32 or as declared, and every sum
+ * is held in fp32 or more.  Rows may lie `ld` elements apart (ld >= their length); elements between them are neither
+ * read nor written.  Arrays need the alignment of their element type only.
+ * --------------------------------------------------------------------------------------------------------------- */
+#define PPO_TOKEN_MAX_VOCAB (1 << 24)
+
+/* Dropout whose mask is a function of (seed, layer, row id, column) and is never stored, so that the pass that collects
+ * a rollout, every later pass over the same samples in any order, and the backward pass drop the same units:
+ *   y = keep ? x * 65536 / (65536 - q) : 0  (+ residual),   q = round(65536 p), 0 <= p <= 1.
+ * Column c of a row with id r is kept where the 16-bit field c % 4 (from the low end) of output c / 4 of the SplitMix64
+ * stream of (seed, layer, r) - the streams that ppo_permutation sorts - is at least q.  A dropped x is not looked at
+ * (NaN included).  d_row_ids: int64 [rows], e.g. flat sample indices; NULL: a row's id is its number.  The backward pass
+ * is the same call on the gradient without d_residual.  d_y may be d_x or d_residual (with the same row stride). */
+int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int64_t ld_x, const int64_t* d_row_ids,
+                const void* d_residual, int64_t ld_residual, double p, uint64_t seed, uint64_t layer, void* d_y, int64_t ld_y,
+                void* hip_stream);
+
+/* Log-probability of the chosen token and entropy of every row of logits, z = logits / temperature:
+ *   logp = z_t - log sum_j exp z_j,   H = -sum_j p_j log p_j   (a term with p_j = 0 counts 0: logits may be -infinity).
+ * d_target int32 [rows].  A row is IDLE if its target lies outside [0, vocab) - its logits are not read then - or if all of
+ * its logits are -infinity: logp and H are 0.  A NaN or +infinity among the logits of any other row gives NaN.
+ * d_entropy may be NULL.  d_stat (may be NULL): fp32 [rows][2], what the backward pass needs of the row. */
+int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab);
+int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target,
+                   float temperature, float* d_logp, float* d_entropy, float* d_stat, void* d_ws, int64_t ws_bytes, void* hip_stream);
+/* Gradient of sum_r (dlogp_r logp_r + dentropy_r H_r) by the logits, rounded once to their type:
+ *   dlogits_j = [dlogp ([j = t] - p_j) - dentropy p_j (log p_j + H)] / temperature;   0 in idle rows.
+ * d_stat and d_entropy as ppo_token_logp left them; d_dentropy NULL (then d_entropy is not read): no entropy term.
+ * d_dlogits may be d_logits (with the same row stride). */
+int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target,
+                            float temperature, const float* d_stat, const float* d_dlogp, const float* d_entropy,
+                            const float* d_dentropy, void* d_dlogits, int64_t ld_d, void* hip_stream);
+
+/* The clipped policy loss on tokens (ppo_update's, for a categorical head) with a KL term against a reference policy, and
+ * its gradient, in one pass over the logits.  With rho = exp(logp - logp_old) and x = logp_ref - logp, a token's loss is
+ *   l = -min(rho A, clip(rho, 1 - clip_lo, 1 + clip_hi) A) + kl_coef (exp x - x - 1) - ent_coef H
+ * (exp x - x - 1: the non-negative one-sample estimate of KL(policy || reference)), and L = scale sum_r weight_r l_r over
+ * the rows that are not idle.  At ties the unclipped branch carries the gradient. */
+typedef struct {
+  float temperature;      /* > 0 */
+  float clip_lo, clip_hi; /* >= 0; clip_lo <= 1 */
+  float kl_coef;          /* >= 0; without d_logp_ref it must be 0 */
+  float ent_coef;         /* 0: the entropy is neither computed nor reported */
+  float scale;            /* e.g. 1 / number of tokens; a loss scale for fp16 gradients */
+} ppo_token_hparams;
+/* Inputs [rows]: d_target, d_logp_old, d_adv; d_logp_ref, d_weight may be NULL (no KL; weights 1).  They are not read in idle
+ * rows.  Outputs: d_dlogits (dL/dlogits; may be d_logits with the same row stride), d_logp [rows] (may be NULL), d_stats [8]:
+ *   0 L, 1..3 its weighted sums scale sum w (-min(..)), scale sum w (exp x - x - 1), scale sum w H, then over the rows that are
+ *   not idle 4 mean of (rho - 1) - log rho, 5 share with rho outside the clip range, 6 their number, 7 1 if L is not finite. */
+int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target,
+                   const float* d_logp_old, const float* d_logp_ref, const float* d_adv, const float* d_weight,
+                   const ppo_token_hparams* hp, void* d_dlogits, int64_t ld_d, float* d_logp, float* d_stats, void* d_ws,
+                   int64_t ws_bytes, void* hip_stream);
+
+/* Sequences of the calls below are packed one behind the other: sequence k holds the tokens [d_offsets[k], d_offsets[k+1])
+ * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty).  Offsets outside [0, tokens] are taken as its
+ * nearer end, and of decreasing ones the results are unspecified; no memory outside the arrays is touched either way.
+ * d_mask: uint8 [tokens], 0 = the token is passed over (a prompt, a tool's answer) and its inputs are not read; NULL: none.
+ *
+ * Preference loss on `pairs` pairs of sequences, k chosen and pairs + k rejected, from the tokens' log-probabilities.
+ * S = sum (logp - logp_ref) over a sequence's unmasked tokens (their mean if length_mean), D = S_chosen - S_rejected:
+ *   kind 0:  l = -(1 - label_smoothing) log sigmoid(beta D) - label_smoothing log sigmoid(-beta D)
+ *   kind 1:  l = (D - 1 / (2 beta))^2
+ * L = scale sum_k l_k over the pairs with an unmasked token in both sequences.  d_logp_ref, d_margin may be NULL.
+ * Outputs: d_dlogp [tokens] (dL/dlogp; 0 for masked tokens and tokens of no sequence), d_margin [pairs] (beta D; 0 for a pair
+ * that does not count), d_stats [7]: 0 L, then over the pairs that count 1 share with D > 0, 2 mean beta D, 3, 4 mean beta S of
+ * the chosen and of the rejected, 5 their number, 6 1 if L is not finite. */
+typedef struct {
+  int32_t kind, length_mean;
+  float beta;            /* > 0 */
+  float label_smoothing; /* in [0, 1]; used by kind 0 */
+  float scale;           /* e.g. 1 / pairs */
+} ppo_pair_hparams;
+int64_t ppo_pair_ws_bytes(int64_t pairs, int64_t tokens);
+int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const float* d_logp_ref, const uint8_t* d_mask,
+                  const int64_t* d_offsets, const ppo_pair_hparams* hp, float* d_dlogp, float* d_margin, float* d_stats,
+                  void* d_ws, int64_t ws_bytes, void* hip_stream);
+
+/* ppo_gae over packed sequences: with ' the next unmasked token of the sequence,
+ *   A_t = r_t + gamma V' - V_t + gamma lambda A',   R_t = A_t + V_t;
+ * behind a sequence's last unmasked token A' = 0 and V' = d_last_value[k] (fp32 [sequences], the value of the state behind a
+ * sequence that was cut off; NULL: 0, every sequence ended).  Masked tokens and tokens of no sequence get 0. */
+int64_t ppo_token_gae_ws_bytes(int64_t sequences, int64_t tokens);
+int ppo_token_gae(int64_t sequences, int64_t tokens, const float* d_reward, const float* d_value, const uint8_t* d_mask,
+                  const int64_t* d_offsets, const float* d_last_value, double gamma, double lambda, float* d_adv, float* d_ret,
+                  void* d_ws, int64_t ws_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,12 +4,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sysconfig
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB = os.path.join(_HERE, "libppo_learner.so")
-SRC = os.path.join(_HERE, "csrc", "ppo_learner.hip")
+# the learner's own path first: its code object is then the first one in the library
+SRCS = [os.path.join(_HERE, "csrc", f) for f in ("ppo_learner.hip", "token_ops.hip")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-Wall", "-Wno-unused-function",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
@@ -41,23 +43,30 @@ def stale() -> bool:
 
 
 def build_lib(force: bool = True, verbose: bool = False) -> str:
-    """Compile the library and the binding, side by side; with force=False only when a source is newer than they are."""
+    """Compile the library's sources and the binding, side by side, and link the library; with force=False only when a source is
+    newer than they are."""
     if force or stale():
-        cmds = {"hipcc": [HIPCC] + FLAGS + ["-o", LIB, SRC], CXX: binding_command()}
-        if verbose:
-            for cmd in cmds.values():
-                print(" ".join(cmd))
-        runs = {n: subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for n, cmd in cmds.items()}
-        # every process is read to its end before any failure is reported: one left with a full pipe never ends
-        errs = {n: "\n".join(l for l in r.communicate()[1].splitlines() if "packed-fp32-ops" not in l) for n, r in runs.items()}
-        failed = [f"{n} failed:\n{errs[n]}" for n, r in runs.items() if r.returncode != 0]
-        if failed:
-            raise RuntimeError("\n".join(failed))
-        if verbose:
-            for err in errs.values():
-                if err.strip():
-                    print(err)
+        with tempfile.TemporaryDirectory() as tmp:
+            objs = {src: os.path.join(tmp, os.path.basename(src) + ".o") for src in SRCS}
+            _run({**{f"{os.path.basename(src)}: hipcc": [HIPCC] + FLAGS + ["-c", "-o", obj, src] for src, obj in objs.items()}, CXX: binding_command()}, verbose)
+            _run({"link: hipcc": [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + list(objs.values())}, verbose)
     return LIB
+
+
+def _run(cmds: dict, verbose: bool):
+    if verbose:
+        for cmd in cmds.values():
+            print(" ".join(cmd))
+    runs = {n: subprocess.Popen(cmd, stdout=subprocess.DEVNULL, stderr=subprocess.PIPE, text=True) for n, cmd in cmds.items()}
+    # every process is read to its end before any failure is reported: one left with a full pipe never ends
+    errs = {n: "\n".join(l for l in r.communicate()[1].splitlines() if "packed-fp32-ops" not in l) for n, r in runs.items()}
+    failed = [f"{n} failed:\n{errs[n]}" for n, r in runs.items() if r.returncode != 0]
+    if failed:
+        raise RuntimeError("\n".join(failed))
+    if verbose:
+        for err in errs.values():
+            if err.strip():
+                print(err)
 
 
 if __name__ == "__main__":

@@ -5,6 +5,7 @@
 #include "../../include/ppo_learner.h"
 #include "common.hip.h"
 #include "gemm.hip.h"
+#include "splitmix.hip.h"
 
 // The per-step scalars of a rollout slab: proprio (-> bf16), action, log-prob, value, reward, done.
 struct ScalarWrite {
@@ -145,25 +146,10 @@ __global__ __launch_bounds__(64) void k_gae(int T, int N, const float* __restric
 }
 
 // ---------------------------------------------------------------- permutation
-// perm = indices sorted by (key_i, i), key_i = i-th output of a SplitMix64 generator whose
+// perm = indices sorted by (key_i, i), key_i = i-th output (perm_key) of a SplitMix64 generator whose
 // state is derived from (seed, update, epoch).  Keys are uniform, so a bucket pass on the top
 // bits followed by an exact rank inside each (small) bucket gives the sorted order without
 // a general sort; the result does not depend on the order of the atomic scatter.
-__host__ __device__ __forceinline__ uint64_t sm64_mix(uint64_t z) {
-  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ULL;
-  z = (z ^ (z >> 27)) * 0x94D049BB133111EBULL;
-  return z ^ (z >> 31);
-}
-__host__ __device__ __forceinline__ uint64_t perm_stream(uint64_t seed, uint64_t update, uint64_t epoch) {
-  const uint64_t G = 0x9E3779B97F4A7C15ULL;
-  uint64_t s = sm64_mix(seed + G);
-  s = sm64_mix(s ^ (update + G));
-  s = sm64_mix(s ^ (epoch + G));
-  return s;
-}
-__device__ __forceinline__ uint64_t perm_key(uint64_t stream, uint64_t i) {
-  return sm64_mix(stream + (i + 1) * 0x9E3779B97F4A7C15ULL);
-}
 __global__ void k_fill_i32(int32_t* p, int64_t n, int32_t v) {
   int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i < n) p[i] = v;

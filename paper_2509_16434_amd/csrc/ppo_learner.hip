@@ -36,6 +36,7 @@
 #include "peaks.hip.h"
 #include "recurrent.hip.h"
 #include "ln0_tile.hip.h"
+#include "static_error.h"
 
 static_assert(sizeof(DevStats) == sizeof(ppo_mb_stats), "device and host statistics records must match");
 
@@ -221,6 +222,12 @@ int fail(Ctx* c, int code, const char* fmt, ...) {
   if (c) c->err = buf; else g_create_error = buf;
   return code;
 }
+
+}  // namespace
+
+int ppo_static_fail(int code, const char* text) { return fail(nullptr, code, "%s", text); }
+
+namespace {
 
 #define HIPCHK(c, call)                                                                          \
   do {                                                                                           \

@@ -1,0 +1,253 @@
+// Host side of the operators without a context for a policy that answers in tokens: argument validation and launches of
+// ppo_dropout, ppo_token_logp(_backward), ppo_token_loss, ppo_pair_loss and ppo_token_gae.
+#include "../../include/ppo_learner.h"
+
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+
+#include <algorithm>
+
+#include "dropout.hip.h"
+#include "static_error.h"
+#include "token_rows.hip.h"
+#include "token_seq.hip.h"
+
+namespace {
+
+int fail(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return ppo_static_fail(code, buf);
+}
+
+#define LAUNCHCHK(what)                                                                                            \
+  do {                                                                                                             \
+    hipError_t e_ = hipGetLastError();                                                                             \
+    if (e_ != hipSuccess) return fail(PPO_EHIP, "launch of %s failed: %s", what, hipGetErrorString(e_));           \
+  } while (0)
+
+constexpr int64_t MAX_ROWS = (int64_t)1 << 30;   // rows, pairs or sequences of one call
+constexpr int64_t MAX_TOKENS = (int64_t)1 << 40;
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+bool finite_in(double v, double lo, double hi) { return v >= lo && v <= hi; }
+bool aligned(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
+int elem_bytes(int32_t dtype) { return dtype == 0 ? 4 : 2; }
+
+// An array of rows: present, aligned to its type, rows that do not overlap.
+int check_rows(const char* name, const void* p, int32_t dtype, int64_t cols, int64_t ld) {
+  if (!p) return fail(PPO_EINVAL, "%s is NULL", name);
+  if (!aligned(p, elem_bytes(dtype))) return fail(PPO_EINVAL, "%s is not aligned to its element type", name);
+  if (ld < cols || ld > MAX_TOKENS) return fail(PPO_ESHAPE, "%s: row stride %lld does not hold rows of %lld", name, (long long)ld, (long long)cols);
+  return PPO_OK;
+}
+int check_array(const char* name, const void* p, int bytes, bool needed) {
+  if (!p && needed) return fail(PPO_EINVAL, "%s is NULL", name);
+  if (p && !aligned(p, bytes)) return fail(PPO_EINVAL, "%s is not aligned to its element type", name);
+  return PPO_OK;
+}
+int check_ws(const void* ws, int64_t have, int64_t want) {
+  if (want == 0) return PPO_OK;
+  if (!ws) return fail(PPO_EINVAL, "d_ws is NULL");
+  if (!aligned(ws, 16)) return fail(PPO_EINVAL, "d_ws is not 16-byte aligned");
+  if (have < want) return fail(PPO_EINVAL, "d_ws has %lld bytes, %lld are needed", (long long)have, (long long)want);
+  return PPO_OK;
+}
+#define CHECK(call)        \
+  do {                     \
+    const int rc_ = (call); \
+    if (rc_) return rc_;   \
+  } while (0)
+
+int check_sizes(int32_t dtype, int64_t rows, int64_t vocab) {
+  if (dtype < 0 || dtype > 2) return fail(PPO_EINVAL, "dtype must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+  if (rows < 0 || rows > MAX_ROWS) return fail(PPO_ESHAPE, "rows must be in [0, %lld] (got %lld)", (long long)MAX_ROWS, (long long)rows);
+  if (vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return fail(PPO_ESHAPE, "vocab must be in [1, %d] (got %lld)", PPO_TOKEN_MAX_VOCAB, (long long)vocab);
+  return PPO_OK;
+}
+
+// f(element type) for the type named by dtype
+template <class F>
+void with_type(int32_t dtype, F f) {
+  if (dtype == 0) f(float());
+  else if (dtype == 1) f(bf16_t());
+  else f(f16_t());
+}
+
+}  // namespace
+
+extern "C" {
+
+int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int64_t ld_x, const int64_t* d_row_ids, const void* d_residual,
+                int64_t ld_residual, double p, uint64_t seed, uint64_t layer, void* d_y, int64_t ld_y, void* hip_stream) {
+  if (dtype < 0 || dtype > 2) return fail(PPO_EINVAL, "dtype must be 0 (fp32), 1 (bf16) or 2 (fp16)");
+  if (rows < 0 || cols < 0 || rows > MAX_ROWS || cols > MAX_ROWS) return fail(PPO_ESHAPE, "rows and columns must be in [0, %lld]", (long long)MAX_ROWS);
+  if (!finite_in(p, 0, 1)) return fail(PPO_EINVAL, "p must be in [0, 1]");
+  if (rows == 0 || cols == 0) return PPO_OK;
+  CHECK(check_rows("d_x", d_x, dtype, cols, ld_x));
+  CHECK(check_rows("d_y", d_y, dtype, cols, ld_y));
+  if (d_residual) CHECK(check_rows("d_residual", d_residual, dtype, cols, ld_residual));
+  CHECK(check_array("d_row_ids", d_row_ids, 8, false));
+  const uint32_t border = (uint32_t)(p * 65536 + 0.5);
+  const DropoutArgs a = {rows, cols, ld_x, ld_residual, ld_y, d_x, d_residual, d_y, d_row_ids, seed, layer, border,
+                         border < 65536 ? 65536.f / (float)(65536 - border) : 0.f};
+  const int grid = (int)std::min<int64_t>(cdiv(rows * cdiv(cols, 4), 256), 1 << 20);
+  with_type(dtype, [&](auto t) { hipLaunchKernelGGL(k_dropout<decltype(t)>, dim3(grid), dim3(256), 0, (hipStream_t)hip_stream, a); });
+  LAUNCHCHK("k_dropout");
+  return PPO_OK;
+}
+
+int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab) {
+  if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return PPO_ESHAPE;
+  return rows * (int64_t)sizeof(LossRecord);
+}
+
+int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, float temperature, float* d_logp,
+                   float* d_entropy, float* d_stat, void* d_ws, int64_t ws_bytes, void* hip_stream) {
+  CHECK(check_sizes(dtype, rows, vocab));
+  if (!(temperature > 0) || !isfinite(temperature) || !isfinite(1.f / temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (rows == 0) return PPO_OK;
+  CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));
+  CHECK(check_array("d_target", d_target, 4, true));
+  CHECK(check_array("d_logp", d_logp, 4, true));
+  CHECK(check_array("d_entropy", d_entropy, 4, false));
+  CHECK(check_array("d_stat", d_stat, 4, false));
+  CHECK(check_ws(d_ws, ws_bytes, ppo_token_ws_bytes(rows, vocab)));
+  RowArgs a = {};
+  a.rows = rows; a.ld = ld; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
+  a.logp = d_logp; a.entropy = d_entropy; a.stat = d_stat;
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (d_entropy) hipLaunchKernelGGL((k_token_logp<T, true>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+    else hipLaunchKernelGGL((k_token_logp<T, false>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+  });
+  LAUNCHCHK("k_token_logp");
+  return PPO_OK;
+}
+
+int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, float temperature,
+                            const float* d_stat, const float* d_dlogp, const float* d_entropy, const float* d_dentropy, void* d_dlogits, int64_t ld_d,
+                            void* hip_stream) {
+  CHECK(check_sizes(dtype, rows, vocab));
+  if (!(temperature > 0) || !isfinite(temperature) || !isfinite(1.f / temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (rows == 0) return PPO_OK;
+  CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));
+  CHECK(check_rows("d_dlogits", d_dlogits, dtype, vocab, ld_d));
+  CHECK(check_array("d_target", d_target, 4, true));
+  CHECK(check_array("d_stat", d_stat, 4, true));
+  CHECK(check_array("d_dlogp", d_dlogp, 4, true));
+  CHECK(check_array("d_dentropy", d_dentropy, 4, false));
+  CHECK(check_array("d_entropy", d_entropy, 4, d_dentropy != nullptr));
+  RowArgs a = {};
+  a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
+  a.stat = (float*)d_stat; a.dlogp = d_dlogp; a.entropy = (float*)d_entropy; a.dentropy = d_dentropy; a.dlogits = d_dlogits;
+  with_type(dtype, [&](auto t) {
+    using T = decltype(t);
+    if (d_dentropy) hipLaunchKernelGGL((k_token_logp_backward<T, true>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+    else hipLaunchKernelGGL((k_token_logp_backward<T, false>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+  });
+  LAUNCHCHK("k_token_logp_backward");
+  return PPO_OK;
+}
+
+int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, const float* d_logp_old,
+                   const float* d_logp_ref, const float* d_adv, const float* d_weight, const ppo_token_hparams* hp, void* d_dlogits, int64_t ld_d,
+                   float* d_logp, float* d_stats, void* d_ws, int64_t ws_bytes, void* hip_stream) {
+  CHECK(check_sizes(dtype, rows, vocab));
+  if (!hp) return fail(PPO_EINVAL, "hp is NULL");
+  if (!(hp->temperature > 0) || !isfinite(hp->temperature) || !isfinite(1.f / hp->temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (!finite_in(hp->clip_lo, 0, 1) || !(hp->clip_hi >= 0) || !isfinite(hp->clip_hi)) return fail(PPO_EINVAL, "clip_lo must be in [0, 1] and clip_hi finite and >= 0");
+  if (!(hp->kl_coef >= 0) || !isfinite(hp->kl_coef)) return fail(PPO_EINVAL, "kl_coef must be finite and >= 0");
+  if (hp->kl_coef > 0 && rows > 0 && !d_logp_ref) return fail(PPO_EINVAL, "kl_coef > 0 needs d_logp_ref");
+  if (!isfinite(hp->ent_coef) || !isfinite(hp->scale)) return fail(PPO_EINVAL, "ent_coef and scale must be finite");
+  CHECK(check_array("d_stats", d_stats, 4, true));
+  if (rows > 0) {
+    CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));
+    CHECK(check_rows("d_dlogits", d_dlogits, dtype, vocab, ld_d));
+    CHECK(check_array("d_target", d_target, 4, true));
+    CHECK(check_array("d_logp_old", d_logp_old, 4, true));
+    CHECK(check_array("d_logp_ref", d_logp_ref, 4, false));
+    CHECK(check_array("d_adv", d_adv, 4, true));
+    CHECK(check_array("d_weight", d_weight, 4, false));
+    CHECK(check_array("d_logp", d_logp, 4, false));
+    CHECK(check_ws(d_ws, ws_bytes, ppo_token_ws_bytes(rows, vocab)));
+  }
+  RowArgs a = {};
+  a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / hp->temperature;
+  a.logp = d_logp; a.dlogits = d_dlogits; a.logp_old = d_logp_old; a.logp_ref = d_logp_ref; a.adv = d_adv; a.weight = d_weight;
+  a.clip_lo = hp->clip_lo; a.clip_hi = hp->clip_hi; a.kl_coef = hp->kl_coef; a.ent_coef = hp->ent_coef; a.scale = hp->scale;
+  a.record = (float*)d_ws;
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (rows > 0) {
+    with_type(dtype, [&](auto t) {
+      using T = decltype(t);
+      if (hp->ent_coef != 0.f) hipLaunchKernelGGL((k_token_loss<T, true>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((k_token_loss<T, false>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+    });
+    LAUNCHCHK("k_token_loss");
+  }
+  hipLaunchKernelGGL(k_token_stats, dim3(1), dim3(1024), 0, st, rows, (const LossRecord*)d_ws, hp->kl_coef, hp->ent_coef, d_stats);
+  LAUNCHCHK("k_token_stats");
+  return PPO_OK;
+}
+
+int64_t ppo_pair_ws_bytes(int64_t pairs, int64_t tokens) {
+  if (pairs < 0 || pairs > MAX_ROWS / 2 || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
+  return pairs * (int64_t)sizeof(PairRecord);
+}
+
+int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const float* d_logp_ref, const uint8_t* d_mask, const int64_t* d_offsets,
+                  const ppo_pair_hparams* hp, float* d_dlogp, float* d_margin, float* d_stats, void* d_ws, int64_t ws_bytes, void* hip_stream) {
+  if (pairs < 0 || pairs > MAX_ROWS / 2 || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "pairs or tokens out of range");
+  if (!hp) return fail(PPO_EINVAL, "hp is NULL");
+  if (hp->kind < 0 || hp->kind > 1) return fail(PPO_EINVAL, "kind must be 0 (sigmoid) or 1 (squared)");
+  if (!(hp->beta > 0) || !isfinite(hp->beta)) return fail(PPO_EINVAL, "beta must be finite and > 0");
+  if (!finite_in(hp->label_smoothing, 0, 1)) return fail(PPO_EINVAL, "label_smoothing must be in [0, 1]");
+  if (!isfinite(hp->scale)) return fail(PPO_EINVAL, "scale must be finite");
+  CHECK(check_array("d_stats", d_stats, 4, true));
+  CHECK(check_array("d_logp", d_logp, 4, tokens > 0));
+  CHECK(check_array("d_logp_ref", d_logp_ref, 4, false));
+  CHECK(check_array("d_dlogp", d_dlogp, 4, tokens > 0));
+  CHECK(check_array("d_margin", d_margin, 4, false));
+  CHECK(check_array("d_offsets", d_offsets, 8, pairs > 0 || tokens > 0));
+  CHECK(check_ws(d_ws, ws_bytes, ppo_pair_ws_bytes(pairs, tokens)));
+  const PairArgs a = {pairs, tokens, d_logp, d_logp_ref, d_mask, d_offsets, hp->kind, hp->length_mean, hp->beta, hp->label_smoothing, hp->scale,
+                      d_dlogp, d_margin, d_stats, (PairRecord*)d_ws};
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (pairs > 0) hipLaunchKernelGGL(k_pair_loss, dim3((uint32_t)pairs), dim3(256), 0, st, a);
+  if (tokens > 0) hipLaunchKernelGGL(k_pair_outside, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 65536)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(k_pair_stats, dim3(1), dim3(1024), 0, st, pairs, (const PairRecord*)d_ws, hp->scale, d_stats);
+  LAUNCHCHK("the kernels of ppo_pair_loss");
+  return PPO_OK;
+}
+
+int64_t ppo_token_gae_ws_bytes(int64_t sequences, int64_t tokens) {
+  if (sequences < 0 || sequences > MAX_ROWS || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
+  return 0;
+}
+
+int ppo_token_gae(int64_t sequences, int64_t tokens, const float* d_reward, const float* d_value, const uint8_t* d_mask, const int64_t* d_offsets,
+                  const float* d_last_value, double gamma, double lambda, float* d_adv, float* d_ret, void* d_ws, int64_t ws_bytes, void* hip_stream) {
+  if (sequences < 0 || sequences > MAX_ROWS || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "sequences or tokens out of range");
+  if (!finite_in(gamma, 0, 1) || !finite_in(lambda, 0, 1)) return fail(PPO_EINVAL, "gamma and lambda must be in [0, 1]");
+  if (tokens == 0) return PPO_OK;
+  CHECK(check_array("d_reward", d_reward, 4, true));
+  CHECK(check_array("d_value", d_value, 4, true));
+  CHECK(check_array("d_offsets", d_offsets, 8, true));
+  CHECK(check_array("d_last_value", d_last_value, 4, false));
+  CHECK(check_array("d_adv", d_adv, 4, true));
+  CHECK(check_array("d_ret", d_ret, 4, true));
+  CHECK(check_ws(d_ws, ws_bytes, ppo_token_gae_ws_bytes(sequences, tokens)));
+  const GaeArgs a = {sequences, tokens, d_reward, d_value, d_last_value, d_mask, d_offsets, gamma, lambda, d_adv, d_ret};
+  hipStream_t st = (hipStream_t)hip_stream;
+  hipLaunchKernelGGL(k_gae_outside, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 65536)), dim3(256), 0, st, a);
+  if (sequences > 0) hipLaunchKernelGGL(k_token_gae, dim3((uint32_t)sequences), dim3(64), 0, st, a);
+  LAUNCHCHK("the kernels of ppo_token_gae");
+  return PPO_OK;
+}
+
+}  // extern "C"

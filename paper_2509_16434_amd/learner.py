@@ -1,5 +1,5 @@
 """Thin binding of libppo_learner.so (see include/ppo_learner.h): ctypes, and for the calls made once per environment
-step the native module _binding (csrc/binding.cpp).
+step, and the operators of a token policy, the native module _binding (csrc/binding.cpp).
 
 Argument marshalling only: every step of the path runs in the library's HIP
 kernels.  PyTorch is used for device memory and the stream, nothing else.  There
@@ -49,10 +49,22 @@ class MbStats(C.Structure):
     _fields_ = [(f, C.c_float) for f in STAT_FIELDS] + [("nonfinite", C.c_int32), ("lr", C.c_float)]
 
 
+class TokenHParams(C.Structure):
+    _fields_ = [(f, C.c_float) for f in ("temperature", "clip_lo", "clip_hi", "kl_coef", "ent_coef", "scale")]
+
+
+class PairHParams(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("length_mean", C.c_int32), ("beta", C.c_float), ("label_smoothing", C.c_float), ("scale", C.c_float)]
+
+
 class LearnerError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{_ERR.get(code, code)}: {msg}")
         self.code = code
+
+
+OPERATORS = ("ppo_dropout", "ppo_token_ws_bytes", "ppo_token_logp", "ppo_token_logp_backward", "ppo_token_loss", "ppo_pair_ws_bytes",
+             "ppo_pair_loss", "ppo_token_gae_ws_bytes", "ppo_token_gae")
 
 
 def load_library():
@@ -88,6 +100,15 @@ def load_library():
         "ppo_update": (C.c_int, [vp, C.POINTER(HParams), C.POINTER(MbStats)]),
         "distill_update": (C.c_int, [vp, C.POINTER(HParams), C.POINTER(MbStats)]),
         "ppo_forward": (C.c_int, [vp, vp, i64, vp, vp]),
+        "ppo_dropout": (C.c_int, [i32, i64, i64, vp, i64, vp, vp, i64, C.c_double, u64, u64, vp, i64, vp]),
+        "ppo_token_ws_bytes": (i64, [i64, i64]),
+        "ppo_token_logp": (C.c_int, [i32, i64, i64, vp, i64, vp, C.c_float, vp, vp, vp, vp, i64, vp]),
+        "ppo_token_logp_backward": (C.c_int, [i32, i64, i64, vp, i64, vp, C.c_float, vp, vp, vp, vp, vp, i64, vp]),
+        "ppo_token_loss": (C.c_int, [i32, i64, i64, vp, i64, vp, vp, vp, vp, vp, C.POINTER(TokenHParams), vp, i64, vp, vp, vp, i64, vp]),
+        "ppo_pair_ws_bytes": (i64, [i64, i64]),
+        "ppo_pair_loss": (C.c_int, [i64, i64, vp, vp, vp, vp, C.POINTER(PairHParams), vp, vp, vp, vp, i64, vp]),
+        "ppo_token_gae_ws_bytes": (i64, [i64, i64]),
+        "ppo_token_gae": (C.c_int, [i64, i64, vp, vp, vp, vp, vp, C.c_double, C.c_double, vp, vp, vp, i64, vp]),
         "ppo_profile": (C.c_int, [vp, i32]),
         "ppo_profile_report": (i64, [vp, C.c_char_p, i64]),
         "ppo_diag_gemm": (C.c_int, [i32, i32, i32, fp, fp, fp]),
@@ -108,7 +129,7 @@ def load_binding(lib):
         raise ImportError(f"the native binding next to {LIB_PATH} is not built ({e}); run `python -c 'import __graft_entry__ as g; g.build()'` "
                           "(or python paper_2509_16434_amd/build.py). There is no fallback path.") from e
     _binding.setup(*(C.cast(getattr(lib, f), C.c_void_p).value for f in
-                     ("ppo_buffer_write", "ppo_buffer_write_range", "ppo_act", "ppo_buffer_write_outcome", "ppo_gae")))
+                     ("ppo_buffer_write", "ppo_buffer_write_range", "ppo_act", "ppo_buffer_write_outcome", "ppo_gae", *OPERATORS)))
     return _binding
 
 
@@ -117,7 +138,7 @@ _native = load_binding(_lib)
 EXPORTS = ("ppo_create", "ppo_destroy", "ppo_last_error", "ppo_param_count", "ppo_buffer_image_bytes",
            "ppo_set_params", "ppo_get_params", "ppo_get_grads", "ppo_set_opt_state", "ppo_get_opt_state", "ppo_get_adaptive_lr", "ppo_set_adaptive_lr",
            "ppo_buffer_write", "ppo_buffer_write_range", "ppo_act", "ppo_buffer_write_outcome", "ppo_buffer_write_state", "ppo_buffer_read_obs", "ppo_gae", "ppo_get_adv_ret", "ppo_permutation", "ppo_permutation_static", "ppo_update", "distill_update",
-           "ppo_forward", "ppo_profile", "ppo_profile_report", "ppo_diag_gemm", "ppo_diag_peak")
+           "ppo_forward", *OPERATORS, "ppo_profile", "ppo_profile_report", "ppo_diag_gemm", "ppo_diag_peak")
 
 
 def make_desc(net: dict, num_envs: int, horizon: int, obs_dtype: str = "bf16", max_chunk: int = 0) -> NetDesc:
@@ -214,6 +235,73 @@ def permutation_static(S: int, seed: int, update_idx: int, epoch: int, out=None,
     if rc:
         raise LearnerError(rc, _lib.ppo_last_error(None).decode())
     return out
+
+
+# ---- operators of a policy that answers in tokens (include/ppo_learner.h has the formulas).  They take CUDA tensors and allocate
+# their results with torch; a matrix may have any row stride.  Work runs on the device of the tensors, on `stream`: None is torch's
+# current stream of that device, and with another one the results belong to it (inputs must be ready on it, as with any stream).
+
+def _on_stream(first, stream, call, *args):
+    import torch
+    if not isinstance(first, torch.Tensor) or not first.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if stream is None:
+        out = call(torch._C._cuda_getCurrentRawStream(first.get_device()), *args)
+    else:
+        if stream.device != first.device:
+            raise ValueError(f"the tensors are on {first.device}, the stream on {stream.device}")
+        with torch.cuda.stream(stream):
+            out = call(stream.cuda_stream, *args)
+    if out[0]:
+        raise LearnerError(out[0], _lib.ppo_last_error(None).decode())
+    return out
+
+
+def dropout(x, p: float, seed: int, layer: int = 0, row_ids=None, residual=None, out=None, stream=None):
+    """ppo_dropout: x [rows][cols] (fp32, bf16, fp16) with the mask of (seed, layer, row id), scaled, plus `residual`; the backward
+    pass is the same call on the gradient without `residual`.  row_ids int64 [rows] (None: row numbers); out may be x or residual."""
+    return _on_stream(x, stream, _native.dropout, x, p, seed, layer, row_ids, residual, out)[1]
+
+
+def token_logp(logits, target, temperature: float = 1.0, want_entropy: bool = False, stream=None):
+    """ppo_token_logp: (logp [rows], entropy [rows] or None, stat [rows][2] for the backward pass) of logits [rows][vocab] at the
+    int32 targets; a target outside [0, vocab) makes a row idle."""
+    return _on_stream(logits, stream, _native.token_logp, logits, target, temperature, want_entropy)[1:]
+
+
+def token_logp_backward(logits, target, stat, dlogp, temperature: float = 1.0, entropy=None, dentropy=None, out=None, stream=None):
+    """ppo_token_logp_backward: gradient of sum(dlogp * logp + dentropy * entropy) by the logits; stat and entropy as token_logp
+    gave them; out may be logits."""
+    return _on_stream(logits, stream, _native.token_logp_backward, logits, target, stat, dlogp, temperature, entropy, dentropy, out)[1]
+
+
+TOKEN_STATS = ("loss", "pi_loss", "kl_ref", "entropy", "approx_kl", "clip_frac", "tokens", "nonfinite")
+
+
+def token_loss(logits, target, logp_old, adv, logp_ref=None, weight=None, scale: float = 1.0, temperature: float = 1.0, clip_lo: float = 0.2,
+               clip_hi: float = 0.2, kl_coef: float = 0.0, ent_coef: float = 0.0, out=None, stream=None):
+    """ppo_token_loss: (dlogits, stats [8] in the order of TOKEN_STATS, logp [rows]); out (for dlogits) may be logits."""
+    return _on_stream(logits, stream, _native.token_loss, logits, target, logp_old, adv, logp_ref, weight, scale, temperature, clip_lo, clip_hi,
+                      kl_coef, ent_coef, out)[1:]
+
+
+PAIR_KINDS = {"sigmoid": 0, "squared": 1}
+PAIR_STATS = ("loss", "accuracy", "margin", "chosen", "rejected", "pairs", "nonfinite")
+
+
+def pair_loss(logp, offsets, logp_ref=None, mask=None, kind: str = "sigmoid", beta: float = 0.1, label_smoothing: float = 0.0,
+              length_mean: bool = False, scale: float = 1.0, stream=None):
+    """ppo_pair_loss: (dlogp [tokens], margin [pairs], stats [7] in the order of PAIR_STATS) of the packed sequences that the int64
+    offsets [2 * pairs + 1] bound, first the chosen ones, then the rejected ones; mask uint8 [tokens]."""
+    if kind not in PAIR_KINDS:
+        raise ValueError(f"kind must be one of {sorted(PAIR_KINDS)}, got {kind!r}")
+    return _on_stream(logp, stream, _native.pair_loss, logp, offsets, logp_ref, mask, PAIR_KINDS[kind], length_mean, beta, label_smoothing, scale)[1:]
+
+
+def token_gae(reward, value, offsets, gamma: float, lam: float, last_value=None, mask=None, stream=None):
+    """ppo_token_gae: (advantages [tokens], returns [tokens]) of the packed sequences that the int64 offsets [sequences + 1] bound;
+    last_value [sequences]: values behind sequences that were cut off; mask uint8 [tokens]."""
+    return _on_stream(reward, stream, _native.token_gae, reward, value, offsets, gamma, lam, last_value, mask)[1:]
 
 
 class Learner:
