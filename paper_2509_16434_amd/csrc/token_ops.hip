@@ -7,6 +7,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dropout.hip.h"
 #include "static_error.h"
@@ -70,12 +71,58 @@ int check_sizes(int32_t dtype, int64_t rows, int64_t vocab) {
   return PPO_OK;
 }
 
+// Rows in slices (k_token_part and what follows it): where whole rows would leave most of the chip idle.
+constexpr int MAX_SLICES = 64;
+int slices_of(int64_t rows, int64_t vocab) {
+  if (rows >= 256 || vocab < 8192) return 1;
+  return (int)std::min<int64_t>(std::min<int64_t>(cdiv(1024, rows), cdiv(vocab, 4096)), MAX_SLICES);
+}
+// slices of a multiple of 64 elements, all but the last of one length, none empty
+void set_slices(RowArgs& a) {
+  const int s = slices_of(a.rows, a.vocab);
+  a.slice_len = (int32_t)(cdiv(cdiv(a.vocab, s), 64) * 64);
+  a.slices = (int32_t)cdiv(a.vocab, a.slice_len);
+}
+
 // f(element type) for the type named by dtype
 template <class F>
 void with_type(int32_t dtype, F f) {
   if (dtype == 0) f(float());
   else if (dtype == 1) f(bf16_t());
   else f(f16_t());
+}
+template <class F>
+void with_flag(bool on, F f) {
+  if (on) f(std::true_type());
+  else f(std::false_type());
+}
+
+// The kernel of a loss: the narrowest group whose registers hold the row.
+template <class T, bool ENT>
+void launch_loss(const RowArgs& a, hipStream_t st) {
+  const int64_t pieces = cdiv(a.vocab, Piece<T>::N);
+  if (a.slices > 1) {
+    hipLaunchKernelGGL((k_token_part<T, ENT>), dim3(a.slices, (uint32_t)a.rows), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_token_loss_slice<T, ENT>), dim3(a.slices, (uint32_t)a.rows), dim3(256), 0, st, a);
+    return;
+  }
+#define LOSS(G, K)                                                                                                                            \
+  if (pieces <= G * K) {                                                                                                                      \
+    hipLaunchKernelGGL((k_token_loss<T, G, K, ENT>), dim3((uint32_t)cdiv(a.rows, G < 256 ? 256 / G : 1)), dim3(G < 256 ? 256 : G), 0, st, a); \
+    return;                                                                                                                                   \
+  }
+  LOSS(16, 2)
+  LOSS(64, 1)
+  LOSS(64, 2)
+  LOSS(64, 4)
+  LOSS(64, 8)
+  LOSS(256, 4)
+  LOSS(256, 8)
+  LOSS(256, 16)
+  LOSS(512, 16)
+  LOSS(1024, 16)
+#undef LOSS
+  hipLaunchKernelGGL((k_token_loss_long<T, ENT>), dim3((uint32_t)a.rows), dim3(1024), 0, st, a);
 }
 
 }  // namespace
@@ -103,7 +150,8 @@ int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int6
 
 int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab) {
   if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return PPO_ESHAPE;
-  return rows * (int64_t)sizeof(LossRecord);
+  const int s = slices_of(std::max<int64_t>(rows, 1), vocab);
+  return (s > 1 ? rows * s * 16 : 0) + rows * (int64_t)sizeof(LossRecord);
 }
 
 int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, float temperature, float* d_logp,
@@ -120,10 +168,21 @@ int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   RowArgs a = {};
   a.rows = rows; a.ld = ld; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
   a.logp = d_logp; a.entropy = d_entropy; a.stat = d_stat;
+  a.part = (float*)d_ws;
+  set_slices(a);
+  hipStream_t st = (hipStream_t)hip_stream;
   with_type(dtype, [&](auto t) {
-    using T = decltype(t);
-    if (d_entropy) hipLaunchKernelGGL((k_token_logp<T, true>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
-    else hipLaunchKernelGGL((k_token_logp<T, false>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+    with_flag(d_entropy != nullptr, [&](auto ent) {
+      using T = decltype(t);
+      constexpr bool ENT = decltype(ent)::value;
+      const int64_t pieces = cdiv(vocab, Piece<T>::N);
+      if (a.slices > 1) {
+        hipLaunchKernelGGL((k_token_part<T, ENT>), dim3(a.slices, (uint32_t)rows), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(k_token_join<ENT>, dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
+      } else if (pieces <= 32) hipLaunchKernelGGL((k_token_logp<T, 16, ENT>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
+      else if (pieces <= 512) hipLaunchKernelGGL((k_token_logp<T, 64, ENT>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((k_token_logp<T, 256, ENT>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+    });
   });
   LAUNCHCHK("k_token_logp");
   return PPO_OK;
@@ -145,10 +204,17 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
   RowArgs a = {};
   a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
   a.stat = (float*)d_stat; a.dlogp = d_dlogp; a.entropy = (float*)d_entropy; a.dentropy = d_dentropy; a.dlogits = d_dlogits;
+  hipStream_t st = (hipStream_t)hip_stream;
   with_type(dtype, [&](auto t) {
-    using T = decltype(t);
-    if (d_dentropy) hipLaunchKernelGGL((k_token_logp_backward<T, true>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
-    else hipLaunchKernelGGL((k_token_logp_backward<T, false>), dim3((uint32_t)rows), dim3(256), 0, (hipStream_t)hip_stream, a);
+    with_flag(d_dentropy != nullptr, [&](auto ent) {
+      using T = decltype(t);
+      constexpr bool ENT = decltype(ent)::value;
+      const int64_t pieces = cdiv(vocab, Piece<T>::N);
+      if (pieces <= 16 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 16, ENT>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
+      else if (pieces <= 64 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 64, ENT>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((k_token_logp_backward<T, 256, ENT>), dim3((uint32_t)cdiv(pieces, 256 * BACK_PIECES), (uint32_t)std::min<int64_t>(rows, 65535), (uint32_t)cdiv(rows, 65535)),
+                              dim3(256), 0, st, a);
+    });
   });
   LAUNCHCHK("k_token_logp_backward");
   return PPO_OK;
@@ -180,17 +246,17 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / hp->temperature;
   a.logp = d_logp; a.dlogits = d_dlogits; a.logp_old = d_logp_old; a.logp_ref = d_logp_ref; a.adv = d_adv; a.weight = d_weight;
   a.clip_lo = hp->clip_lo; a.clip_hi = hp->clip_hi; a.kl_coef = hp->kl_coef; a.ent_coef = hp->ent_coef; a.scale = hp->scale;
-  a.record = (float*)d_ws;
   hipStream_t st = (hipStream_t)hip_stream;
   if (rows > 0) {
+    set_slices(a);
+    a.part = (float*)d_ws;
+    a.record = (float*)d_ws + (a.slices > 1 ? rows * a.slices * 4 : 0);
     with_type(dtype, [&](auto t) {
-      using T = decltype(t);
-      if (hp->ent_coef != 0.f) hipLaunchKernelGGL((k_token_loss<T, true>), dim3((uint32_t)rows), dim3(256), 0, st, a);
-      else hipLaunchKernelGGL((k_token_loss<T, false>), dim3((uint32_t)rows), dim3(256), 0, st, a);
+      with_flag(hp->ent_coef != 0.f, [&](auto ent) { launch_loss<decltype(t), decltype(ent)::value>(a, st); });
     });
     LAUNCHCHK("k_token_loss");
   }
-  hipLaunchKernelGGL(k_token_stats, dim3(1), dim3(1024), 0, st, rows, (const LossRecord*)d_ws, hp->kl_coef, hp->ent_coef, d_stats);
+  hipLaunchKernelGGL(k_token_stats, dim3(1), dim3(1024), 0, st, rows, (const LossRecord*)a.record, hp->kl_coef, hp->ent_coef, d_stats);
   LAUNCHCHK("k_token_stats");
   return PPO_OK;
 }

@@ -4,9 +4,12 @@
 //   z = x / temperature, m = max z, s = sum exp(z - m), p = exp(z - m) / s
 //   logp = z_t - m - log s,   H = log s - sum p (z - m)
 //   d/dx of g logp + h H:   [ g ([j = t] - p_j) - h p_j (log p_j + H) ] / temperature
-// The kernels work with d = x - max x (exact to one fp32 rounding whatever the size of x) and e = exp2(d * log2(e) / temperature).
+// The kernels work with d = x - max x (exact to one fp32 rounding whatever the size of x) and e = exp2(d c), c = log2(e) / temperature.
 // A row is idle when its target is outside [0, vocab) (its logits are not read then) or none of its logits is above -infinity:
 // log-probability, entropy and terms of the loss 0, gradient row 0.
+//
+// All of it is bound by memory: 2 or 4 bytes a logit once in and, for a gradient, once out.  A row is worked on by G threads that
+// hold 16-byte pieces of it; rows of any alignment are read and written in such pieces (the hardware takes them at any address).
 #pragma once
 #include "elem.hip.h"
 
@@ -23,155 +26,476 @@ struct RowArgs {
   const float *logp_old, *logp_ref, *adv, *weight;    // loss (logp_ref, weight: may be NULL)
   float clip_lo, clip_hi, kl_coef, ent_coef, scale;
   float* record;                                      // loss: LossRecord per row
+  float* part;                                        // rows in slices: PartStat per row and slice
+  int32_t slices, slice_len;
 };
 
 // What a row adds to the statistics of the loss.
 struct LossRecord { float pi, kl, ent, old_kl, clipped, active; };
 
-struct RowStat { float mx, s, sd; };  // max x; sum e; sum e d
-
-__device__ __forceinline__ float block_max(float v, float* lds) {
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = lds[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v = fmaxf(v, lds[w]);
-  __syncthreads();
-  return v;
-}
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = lds[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v += lds[w];
-  __syncthreads();
-  return v;
-}
+// max x, sum e, sum e d (with respect to the max; to 0 where it is -infinity).  idle(): nothing above -infinity, and no NaN.
+struct RowStat {
+  float mx, s, sd;
+  __device__ __forceinline__ float base() const { return mx == -INFINITY ? 0.f : mx; }
+  __device__ __forceinline__ bool idle() const { return mx == -INFINITY && s == 0.f; }
+};
 
 #define TOKEN_LOG2E 1.44269504088896340736f
+#define TOKEN_LN2 0.69314718055994530942f
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }  // 1 ulp; results below 2^-126 are 0
 // d of a logit of -infinity is -infinity: as a factor it is held at a finite value, so that 0 * d stays 0
 __device__ __forceinline__ float finite_d(float d) { return fmaxf(d, -1e30f); }
 
+// ---- over the lanes of a wave: within 16 lanes by permutations of the operand, then across
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+#define DPP_XOR1 0xB1         // quad_perm [1,0,3,2]
+#define DPP_XOR2 0x4E         // quad_perm [2,3,0,1]
+#define DPP_HALF_MIRROR 0x141
+#define DPP_MIRROR 0x140
+// over groups of W = 16 or 64 lanes
+template <int W> __device__ __forceinline__ float lanes_max(float v) {
+  v = fmaxf(v, dpp<DPP_XOR1>(v)); v = fmaxf(v, dpp<DPP_XOR2>(v));
+  v = fmaxf(v, dpp<DPP_HALF_MIRROR>(v)); v = fmaxf(v, dpp<DPP_MIRROR>(v));
+  if (W == 64) { v = fmaxf(v, __shfl_xor(v, 16)); v = fmaxf(v, __shfl_xor(v, 32)); }
+  return v;
+}
+template <int W> __device__ __forceinline__ float lanes_sum(float v) {
+  v += dpp<DPP_XOR1>(v); v += dpp<DPP_XOR2>(v); v += dpp<DPP_HALF_MIRROR>(v); v += dpp<DPP_MIRROR>(v);
+  if (W == 64) { v += __shfl_xor(v, 16); v += __shfl_xor(v, 32); }
+  return v;
+}
+
+// ---- statistics of parts of a row, joined
+// b's sums with respect to the maximum mx (>= b.mx)
+template <bool ENT>
+__device__ __forceinline__ RowStat rebase(RowStat b, float mx, float c) {
+  const bool none = b.mx == -INFINITY;   // sums 0 (or NaN): no factor
+  const float d = none ? 0.f : b.mx - mx, f = exp2_hw(d * c);
+  if (ENT) b.sd = f * (b.sd + b.s * finite_d(d));
+  b.s *= f;
+  b.mx = mx;
+  return b;
+}
+// the threads of a row's group; r: the thread's own part, on return the row's.  lds: 3 floats per wave of the block; one barrier
+// (G <= 64: neither).
+template <int G, bool ENT>
+__device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
+  constexpr int W = G < 64 ? G : 64;
+  RowStat w = rebase<ENT>(r, lanes_max<W>(r.mx), c);
+  w.s = lanes_sum<W>(w.s);
+  if (ENT) w.sd = lanes_sum<W>(w.sd);
+  if constexpr (G <= 64) return w;
+  else {
+  constexpr int NW = G / 64;
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) { lds[3 * wave] = w.mx; lds[3 * wave + 1] = w.s; if (ENT) lds[3 * wave + 2] = w.sd; }
+  __syncthreads();
+  float mx = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < NW; ++k) mx = fmaxf(mx, lds[3 * k]);
+  RowStat all = {mx, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < NW; ++k) {
+    const RowStat p = rebase<ENT>(RowStat{lds[3 * k], lds[3 * k + 1], ENT ? lds[3 * k + 2] : 0.f}, mx, c);
+    all.s += p.s;
+    if (ENT) all.sd += p.sd;
+  }
+  return all;
+  }
+}
+
+// ---- 16 bytes of a row
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
+template <class T> struct Piece { static constexpr int N = 16 / sizeof(T); };
+template <class T> __device__ __forceinline__ u32x4_t load_piece(const T* p) { return *reinterpret_cast<const u32x4_any_t*>(p); }
+template <class T> __device__ __forceinline__ void store_piece(T* p, u32x4_t v) { *reinterpret_cast<u32x4_any_t*>(p) = v; }
+__device__ __forceinline__ void unpack(u32x4_t v, float (&f)[4], float) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+}
+__device__ __forceinline__ void unpack(u32x4_t v, float (&f)[8], bf16_t) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(v[i] << 16); f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void unpack(u32x4_t v, float (&f)[8], f16_t) {
+  typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t w = v[i];  // a copy: the cast of a vector's element itself takes element 0
+    const h2_t h = __builtin_bit_cast(h2_t, w);
+    f[2 * i] = (float)h[0]; f[2 * i + 1] = (float)h[1];
+  }
+}
+__device__ __forceinline__ u32x4_t pack(const float (&f)[4], float) {
+  u32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+  return v;
+}
+__device__ __forceinline__ u32x4_t pack(const float (&f)[8], bf16_t) {
+  u32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = pack2bf(f[2 * i], f[2 * i + 1]);
+  return v;
+}
+__device__ __forceinline__ u32x4_t pack(const float (&f)[8], f16_t) {
+  typedef _Float16 h2_t __attribute__((ext_vector_type(2)));
+  u32x4_t v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { const h2_t h = {(_Float16)f[2 * i], (_Float16)f[2 * i + 1]}; v[i] = __builtin_bit_cast(uint32_t, h); }
+  return v;
+}
+// two lowest-valued logits, for the places behind the end of a row
+__device__ __forceinline__ uint32_t no_logits(float) { return 0xff800000u; }
+__device__ __forceinline__ uint32_t no_logits(bf16_t) { return 0xff80ff80u; }
+__device__ __forceinline__ uint32_t no_logits(f16_t) { return 0xfc00fc00u; }
+// elements i .. i + N - 1 of a row (or part) of n elements; those behind its end are -infinity
+template <class T>
+__device__ __forceinline__ u32x4_t load_row(const T* x, int i, int n) {
+  constexpr int N = Piece<T>::N;
+  const uint32_t none = no_logits(T());
+  u32x4_t v = {none, none, none, none};
+  if (i + N <= n) v = load_piece(x + i);
+  else if (i < n) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (i + k < n) {
+        if constexpr (sizeof(T) == 4) v[k] = __float_as_uint(x[i + k]);
+        else { const T one = x[i + k]; const uint32_t h = __builtin_bit_cast(uint16_t, one); v[k >> 1] = k & 1 ? (v[k >> 1] & 0xffffu) | (h << 16) : (v[k >> 1] & 0xffff0000u) | h; }
+      }
+    }
+  }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ void store_row(T* y, int i, int n, u32x4_t v) {
+  constexpr int N = Piece<T>::N;
+  if (i + N <= n) store_piece(y + i, v);
+  else if (i < n) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (i + k < n) {
+        if constexpr (sizeof(T) == 4) y[i + k] = __uint_as_float(v[k]);
+        else { const uint16_t h = (uint16_t)(v[k >> 1] >> (k & 1 ? 16 : 0)); y[i + k] = __builtin_bit_cast(T, h); }
+      }
+    }
+  }
+}
+
+// adds a piece's terms to r, whose maximum covers them
 template <class T, bool ENT>
-__device__ __forceinline__ RowStat row_stat(const T* x, int V, float inv_t, float* lds) {
-  RowStat r;
-  float mx = -INFINITY, bad = 0.f;
-  for (int i = threadIdx.x; i < V; i += blockDim.x) {
-    const float v = to_f(x[i]);
-    mx = fmaxf(mx, v);
-    bad += v != v ? 1.f : 0.f;
+__device__ __forceinline__ void add_piece(RowStat& r, u32x4_t v, float base, float c) {
+  float f[Piece<T>::N];
+  unpack(v, f, T());
+#pragma unroll
+  for (int k = 0; k < Piece<T>::N; ++k) {
+    const float d = f[k] - base, e = exp2_hw(d * c);
+    r.s += e;
+    if (ENT) r.sd += e * finite_d(d);
   }
-  r.mx = block_max(mx, lds);
-  if (block_sum(bad, lds) > 0.f) r.mx = NAN;   // a row of NaN and -infinity is not an idle one
-  float s = 0.f, sd = 0.f;
-  for (int i = threadIdx.x; i < V; i += blockDim.x) {
-    const float d = to_f(x[i]) - r.mx, e = exp2f(d * (inv_t * TOKEN_LOG2E));
-    s += e;
-    if (ENT) sd += e * finite_d(d);
+}
+template <class T>
+__device__ __forceinline__ float max_piece(u32x4_t v) {
+  float f[Piece<T>::N], m;
+  unpack(v, f, T());
+  m = f[0];
+#pragma unroll
+  for (int k = 1; k < Piece<T>::N; ++k) m = fmaxf(m, f[k]);
+  return m;
+}
+
+// The statistics of n elements by G threads in one pass: every thread keeps its own maximum and sums, brought to a new maximum
+// U pieces at a time, so that U loads are in flight and one exponential in 8 U (or 4 U) is for that.
+template <class T, int G, bool ENT>
+__device__ __forceinline__ RowStat stream_stat(const T* x, int n, int tid, float c) {
+  constexpr int N = Piece<T>::N, U = 4;
+  RowStat r = {-INFINITY, 0.f, 0.f};
+  for (int i = tid * N; i < n; i += G * N * U) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, n);
+    float m = r.mx;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = fmaxf(m, max_piece<T>(v[u]));
+    r = rebase<ENT>(r, m, c);
+    const float base = r.base();
+#pragma unroll
+    for (int u = 0; u < U; ++u) add_piece<T, ENT>(r, v[u], base, c);
   }
-  r.s = block_sum(s, lds);
-  r.sd = ENT ? block_sum(sd, lds) : 0.f;
   return r;
 }
 
-template <class T, bool ENT>
-__global__ __launch_bounds__(256) void k_token_logp(RowArgs a) {
-  __shared__ float lds[16];
-  const int64_t row = blockIdx.x;
+struct RowOut { float logp, ent, ls; };
+__device__ __forceinline__ RowOut row_out(const RowStat& r, float xt, float inv_t, bool ent) {
+  RowOut o;
+  o.ls = logf(r.s);
+  o.logp = (xt - r.base()) * inv_t - o.ls;
+  o.ent = ent ? o.ls - r.sd / r.s * inv_t : 0.f;
+  return o;
+}
+// Log-probability (and entropy) of rows by groups of G threads.
+template <class T, int G, bool ENT>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_logp(RowArgs a) {
+  constexpr int NT = G < 256 ? 256 : G;
+  __shared__ float lds[3 * (NT / 64)];
+  const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);
+  if (G < 256 && row >= a.rows) return;   // G <= 64: no barrier follows
   const int t = a.target[row];
+  const float c = a.inv_t * TOKEN_LOG2E;
   const T* x = (const T*)a.logits + row * a.ld;
-  float logp = 0.f, ent = 0.f, st0 = 0.f, st1 = 0.f;
+  RowOut o = {0.f, 0.f, 0.f};
+  float mx = -INFINITY;
   if (t >= 0 && t < a.vocab) {
-    const RowStat r = row_stat<T, ENT>(x, a.vocab, a.inv_t, lds);
-    if (r.mx != -INFINITY) {
-      const float ls = logf(r.s);
-      logp = (to_f(x[t]) - r.mx) * a.inv_t - ls;
-      ent = ls - r.sd / r.s * a.inv_t;
-      st0 = r.mx; st1 = ls;
-    } else { st0 = -INFINITY; }
+    const float xt = to_f(x[t]);
+    const RowStat r = group_join<G, ENT>(stream_stat<T, G, ENT>(x, a.vocab, threadIdx.x % G, c), c, lds);
+    if (!r.idle()) { o = row_out(r, xt, a.inv_t, ENT); mx = r.base(); }
   }
-  if (threadIdx.x == 0) {
-    a.logp[row] = logp;
-    if (a.entropy) a.entropy[row] = ent;
-    if (a.stat) { a.stat[2 * row] = st0; a.stat[2 * row + 1] = st1; }
+  if (threadIdx.x % G == 0) {
+    a.logp[row] = o.logp;
+    if (a.entropy) a.entropy[row] = o.ent;
+    if (a.stat) { a.stat[2 * row] = mx; a.stat[2 * row + 1] = o.ls; }
   }
 }
 
-// gradient row: -e (k0 + k1 d) and, at the target, + add
+// Few long rows: statistics of slices of a row, one block each.
 template <class T, bool ENT>
-__device__ __forceinline__ void row_gradient(const T* x, T* y, int V, int t, float mx, float c, float k0, float k1, float add) {
-  for (int i = threadIdx.x; i < V; i += blockDim.x) {
-    const float d = to_f(x[i]) - mx, e = exp2f(d * c);
-    float g = -e * (ENT ? k0 + k1 * finite_d(d) : k0);
-    if (i == t) g += add;
-    y[i] = from_f<T>(g);
-  }
-}
-
-template <class T, bool ENT>
-__global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
-  const int64_t row = blockIdx.x;
+__global__ __launch_bounds__(256) void k_token_part(RowArgs a) {
+  __shared__ float lds[12];
+  const int64_t row = blockIdx.y;
   const int t = a.target[row];
+  if (t < 0 || t >= a.vocab) return;   // nobody reads the parts of such a row
+  const float c = a.inv_t * TOKEN_LOG2E;
+  const int from = blockIdx.x * a.slice_len, n = min(a.vocab - from, a.slice_len);
+  const RowStat r = group_join<256, ENT>(stream_stat<T, 256, ENT>((const T*)a.logits + row * a.ld + from, n, threadIdx.x, c), c, lds);
+  if (threadIdx.x == 0) *(float4*)(a.part + 4 * (row * a.slices + blockIdx.x)) = make_float4(r.mx, r.s, r.sd, blockIdx.x == 0 ? to_f(((const T*)a.logits)[row * a.ld + t]) : 0.f);
+}
+// the parts of a row (at most 64), joined by one wave
+template <bool ENT>
+__device__ __forceinline__ RowStat join_parts(const RowArgs& a, int64_t row, float c) {
+  const int lane = threadIdx.x & 63;
+  RowStat r = {-INFINITY, 0.f, 0.f};
+  if (lane < a.slices) { const float4 p = *(const float4*)(a.part + 4 * (row * a.slices + lane)); r = RowStat{p.x, p.y, p.z}; }
+  return group_join<64, ENT>(r, c, nullptr);
+}
+template <bool ENT>
+__global__ __launch_bounds__(256) void k_token_join(RowArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.rows) return;
+  const int t = a.target[row];
+  RowOut o = {0.f, 0.f, 0.f};
+  float mx = -INFINITY;
+  if (t >= 0 && t < a.vocab) {
+    const RowStat r = join_parts<ENT>(a, row, a.inv_t * TOKEN_LOG2E);
+    if (!r.idle()) { o = row_out(r, a.part[4 * row * a.slices + 3], a.inv_t, ENT); mx = r.base(); }
+  }
+  if ((threadIdx.x & 63) == 0) {
+    a.logp[row] = o.logp;
+    if (a.entropy) a.entropy[row] = o.ent;
+    if (a.stat) { a.stat[2 * row] = mx; a.stat[2 * row + 1] = o.ls; }
+  }
+}
+
+// ---- gradient: -e (k0 + k1 d), and `add` more at the target
+struct GradCoef { float mx, c, k0, k1, add; };
+// g: dL/dlogp, h: dL/dH; is = 1 / (s temperature)
+__device__ __forceinline__ GradCoef grad_coef(float g, float h, float ent, float ls, float mx, float is, float inv_t) {
+  return GradCoef{mx, inv_t * TOKEN_LOG2E, (g + h * (ent - ls)) * is, h * inv_t * is, g * inv_t};
+}
+// t: the target's place in the piece, if it is in it
+template <class T, bool ENT>
+__device__ __forceinline__ u32x4_t grad_piece(u32x4_t v, const GradCoef& k, int t) {
+  constexpr int N = Piece<T>::N;
+  float f[N];
+  unpack(v, f, T());
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = f[i] - k.mx, e = exp2_hw(d * k.c);
+    f[i] = -e * (ENT ? k.k0 + k.k1 * finite_d(d) : k.k0);
+  }
+  if ((unsigned)t < (unsigned)N) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] += i == t ? k.add : 0.f;
+  }
+  return pack(f, T());
+}
+template <class T>
+__device__ __forceinline__ void zero_row(T* y, int n, int tid, int G) {
+  const u32x4_t z = {0, 0, 0, 0};
+  for (int i = tid * Piece<T>::N; i < n; i += G * Piece<T>::N) store_row(y, i, n, z);
+}
+
+// Gradient of the log-probability and the entropy from the row's statistics: every piece by itself.  A group of G threads does a
+// slice of G BACK_PIECES pieces of a row: blockIdx.x the slice (G < 256: the row is one slice), blockIdx.y and z the row.
+constexpr int BACK_PIECES = 4;
+template <class T, int G, bool ENT>
+__global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
+  constexpr int N = Piece<T>::N;
+  const int64_t row = G < 256 ? (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G : blockIdx.y + (int64_t)blockIdx.z * 65535;
+  if (row >= a.rows) return;
+  const int t = a.target[row], from = (G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N)) + threadIdx.x % G * N;
   const T* x = (const T*)a.logits + row * a.ld;
   T* y = (T*)a.dlogits + row * a.ldd;
   const float mx = a.stat[2 * row], ls = a.stat[2 * row + 1];
+  const u32x4_t z = {0, 0, 0, 0};
   if (t < 0 || t >= a.vocab || mx == -INFINITY) {
-    for (int i = threadIdx.x; i < a.vocab; i += 256) y[i] = from_f<T>(0.f);
+#pragma unroll
+    for (int u = 0; u < BACK_PIECES; ++u) store_row(y, from + u * G * N, a.vocab, z);
     return;
   }
   const float g = a.dlogp[row], h = ENT ? a.dentropy[row] : 0.f, H = ENT ? a.entropy[row] : 0.f;
-  const float is = expf(-ls) * a.inv_t;
-  row_gradient<T, ENT>(x, y, a.vocab, t, mx, a.inv_t * TOKEN_LOG2E, (g + h * (H - ls)) * is, h * a.inv_t * is, g * a.inv_t);
+  const GradCoef k = grad_coef(g, h, H, ls, mx, expf(-ls) * a.inv_t, a.inv_t);
+  u32x4_t v[BACK_PIECES];
+#pragma unroll
+  for (int u = 0; u < BACK_PIECES; ++u) v[u] = load_row(x, from + u * G * N, a.vocab);
+#pragma unroll
+  for (int u = 0; u < BACK_PIECES; ++u) store_row(y, from + u * G * N, a.vocab, grad_piece<T, ENT>(v[u], k, t - (from + u * G * N)));
 }
 
+// ---- loss
 // Terms of the loss at one token and their derivatives by logp (g) and H (h), all without weight.
 struct LossTerm { float g, h; LossRecord rec; };
-__device__ __forceinline__ LossTerm loss_term(const RowArgs& a, int64_t row, float logp, float ent) {
+struct LossIn { float old, ref, adv, w; };
+__device__ __forceinline__ LossIn loss_in(const RowArgs& a, int64_t row) {
+  return LossIn{a.logp_old[row], a.logp_ref ? a.logp_ref[row] : 0.f, a.adv[row], (a.weight ? a.weight[row] : 1.f) * a.scale};
+}
+__device__ __forceinline__ LossTerm loss_term(const RowArgs& a, const LossIn& in, float logp, float ent) {
   LossTerm o;
-  const float adv = a.adv[row], lr = logp - a.logp_old[row], rho = expf(lr);
+  const float lr = logp - in.old, rho = expf(lr);
   const float lo = 1.f - a.clip_lo, hi = 1.f + a.clip_hi;
-  const float s1 = rho * adv, s2 = fminf(fmaxf(rho, lo), hi) * adv;
+  const float s1 = rho * in.adv, s2 = fminf(fmaxf(rho, lo), hi) * in.adv;
   const bool held = s1 > s2;  // ties: the unclipped branch carries the gradient; so does a NaN, which is to be seen in the loss
-  o.rec.pi = held ? -s2 : -s1;
+  o.rec.pi = (held ? -s2 : -s1) * in.w;
   o.g = held ? 0.f : -s1;
   o.rec.kl = 0.f;
   if (a.logp_ref) {
-    const float d = a.logp_ref[row] - logp, ed = expf(d);
-    o.rec.kl = ed - d - 1.f;
+    const float d = in.ref - logp, ed = expf(d);
+    o.rec.kl = (ed - d - 1.f) * in.w;
     o.g += a.kl_coef * (1.f - ed);
   }
-  o.rec.ent = ent;
+  o.rec.ent = ent * in.w;
   o.h = -a.ent_coef;
   o.rec.old_kl = (rho - 1.f) - lr;
   o.rec.clipped = rho < lo || rho > hi ? 1.f : 0.f;
   o.rec.active = 1.f;
+  o.g *= in.w; o.h *= in.w;
   return o;
 }
+__device__ __forceinline__ GradCoef loss_row(const RowArgs& a, int64_t row, const LossIn& in, const RowStat& r, float xt, bool ent, bool writes) {
+  const RowOut o = row_out(r, xt, a.inv_t, ent);
+  const LossTerm l = loss_term(a, in, o.logp, o.ent);
+  if (writes) {
+    if (a.logp) a.logp[row] = o.logp;
+    ((LossRecord*)a.record)[row] = l.rec;
+  }
+  return grad_coef(l.g, l.h, o.ent, o.ls, r.base(), a.inv_t / r.s, a.inv_t);
+}
+__device__ __forceinline__ void loss_idle(const RowArgs& a, int64_t row) {
+  if (a.logp) a.logp[row] = 0.f;
+  ((LossRecord*)a.record)[row] = LossRecord{0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+}
 
+// Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers between the pass that
+// adds up and the one that writes, so that memory sees it once in and once out.
+template <class T, int G, int K, bool ENT>
+__global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_loss(RowArgs a) {
+  constexpr int NT = G < 256 ? 256 : G, N = Piece<T>::N;
+  __shared__ float lds[3 * (NT / 64)];
+  const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);
+  if (G < 256 && row >= a.rows) return;   // G <= 64: no barrier follows
+  const int t = a.target[row], tid = threadIdx.x % G, at = tid * N;
+  const T* x = (const T*)a.logits + row * a.ld;
+  T* y = (T*)a.dlogits + row * a.ldd;
+  if (t < 0 || t >= a.vocab) {
+    zero_row(y, a.vocab, tid, G);
+    if (tid == 0) loss_idle(a, row);
+    return;
+  }
+  const float c = a.inv_t * TOKEN_LOG2E;
+  const LossIn in = loss_in(a, row);
+  float xt = to_f(x[t]);
+  u32x4_t v[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = load_row(x, at + k * G * N, a.vocab);
+  asm volatile("" : "+v"(xt));   // read before the barrier: the gradient may lie in the logits' memory
+  float m = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < K; ++k) m = fmaxf(m, max_piece<T>(v[k]));
+  RowStat r = {lanes_max<G < 64 ? G : 64>(m), 0.f, 0.f};
+  const float base = r.base();
+#pragma unroll
+  for (int k = 0; k < K; ++k) add_piece<T, ENT>(r, v[k], base, c);
+  r = group_join<G, ENT>(r, c, lds);
+  if (r.idle()) {
+    zero_row(y, a.vocab, tid, G);
+    if (tid == 0) loss_idle(a, row);
+    return;
+  }
+  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
+#pragma unroll
+  for (int k = 0; k < K; ++k) store_row(y, at + k * G * N, a.vocab, grad_piece<T, ENT>(v[k], q, t - (at + k * G * N)));
+}
+
+// Longer rows: read twice by a block.
 template <class T, bool ENT>
-__global__ __launch_bounds__(256) void k_token_loss(RowArgs a) {
-  __shared__ float lds[16];
+__global__ __launch_bounds__(1024) void k_token_loss_long(RowArgs a) {
+  constexpr int N = Piece<T>::N, G = 1024, U = 4;
+  __shared__ float lds[3 * (G / 64)];
   const int64_t row = blockIdx.x;
-  const int t = a.target[row];
+  const int t = a.target[row], tid = threadIdx.x;
   const T* x = (const T*)a.logits + row * a.ld;
   T* y = (T*)a.dlogits + row * a.ldd;
   RowStat r = {-INFINITY, 0.f, 0.f};
-  if (t >= 0 && t < a.vocab) r = row_stat<T, ENT>(x, a.vocab, a.inv_t, lds);
-  if (r.mx == -INFINITY) {
-    for (int i = threadIdx.x; i < a.vocab; i += 256) y[i] = from_f<T>(0.f);
-    if (threadIdx.x == 0) { a.logp[row] = 0.f; ((LossRecord*)a.record)[row] = LossRecord{0.f, 0.f, 0.f, 0.f, 0.f, 0.f}; }
+  const float c = a.inv_t * TOKEN_LOG2E;
+  float xt = 0.f;
+  LossIn in;
+  if (t >= 0 && t < a.vocab) {
+    in = loss_in(a, row);
+    xt = to_f(x[t]);
+    asm volatile("" : "+v"(xt));
+    r = group_join<G, ENT>(stream_stat<T, G, ENT>(x, a.vocab, tid, c), c, lds);
+  }
+  if (r.idle()) {
+    zero_row(y, a.vocab, tid, G);
+    if (tid == 0) loss_idle(a, row);
     return;
   }
-  const float ls = logf(r.s), logp = (to_f(x[t]) - r.mx) * a.inv_t - ls, H = ENT ? ls - r.sd / r.s * a.inv_t : 0.f;
-  LossTerm o = loss_term(a, row, logp, H);
-  const float w = (a.weight ? a.weight[row] : 1.f) * a.scale, g = w * o.g, h = w * o.h, is = a.inv_t / r.s;
-  __syncthreads();  // x[t] is read: the gradient may lie in the memory of the logits
-  row_gradient<T, ENT>(x, y, a.vocab, t, r.mx, a.inv_t * TOKEN_LOG2E, (g + h * (H - ls)) * is, h * a.inv_t * is, g * a.inv_t);
-  if (threadIdx.x == 0) {
-    a.logp[row] = logp;
-    o.rec.pi *= w; o.rec.kl *= w; o.rec.ent *= w;
-    ((LossRecord*)a.record)[row] = o.rec;
+  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
+  for (int i = tid * N; i < a.vocab; i += G * N * U) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, a.vocab);
+#pragma unroll
+    for (int u = 0; u < U; ++u) store_row(y, i + u * G * N, a.vocab, grad_piece<T, ENT>(v[u], q, t - (i + u * G * N)));
+  }
+}
+
+// Few long rows: k_token_part has left the statistics of the slices; every slice's block joins them all and writes its gradient.
+// The target's logit may be overwritten by the block that owns it before another has read it: part 0's spare place holds it.
+template <class T, bool ENT>
+__global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
+  constexpr int N = Piece<T>::N, G = 256, U = 4;
+  const int64_t row = blockIdx.y;
+  const int t = a.target[row], tid = threadIdx.x, from = blockIdx.x * a.slice_len, n = min(a.vocab - from, a.slice_len);
+  const T* x = (const T*)a.logits + row * a.ld + from;
+  T* y = (T*)a.dlogits + row * a.ldd + from;
+  const bool first = blockIdx.x == 0 && tid == 0;
+  RowStat r = {-INFINITY, 0.f, 0.f};
+  if (t >= 0 && t < a.vocab) r = join_parts<ENT>(a, row, a.inv_t * TOKEN_LOG2E);
+  if (r.idle()) {
+    zero_row(y, n, tid, G);
+    if (first) loss_idle(a, row);
+    return;
+  }
+  const GradCoef q = loss_row(a, row, loss_in(a, row), r, a.part[4 * row * a.slices + 3], ENT, first);
+  for (int i = tid * N; i < n; i += G * N * U) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, n);
+#pragma unroll
+    for (int u = 0; u < U; ++u) store_row(y, i + u * G * N, n, grad_piece<T, ENT>(v[u], q, t - (from + i + u * G * N)));
   }
 }
 
