@@ -92,16 +92,13 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) { lds[3 * wave] = w.mx; lds[3 * wave + 1] = w.s; if (ENT) lds[3 * wave + 2] = w.sd; }
   __syncthreads();
-  float mx = -INFINITY;
-#pragma unroll
-  for (int k = 0; k < NW; ++k) mx = fmaxf(mx, lds[3 * k]);
-  RowStat all = {mx, 0.f, 0.f};
-#pragma unroll
-  for (int k = 0; k < NW; ++k) {
-    const RowStat p = rebase<ENT>(RowStat{lds[3 * k], lds[3 * k + 1], ENT ? lds[3 * k + 2] : 0.f}, mx, c);
-    all.s += p.s;
-    if (ENT) all.sd += p.sd;
-  }
+  // every 16 lanes read the (at most 16) waves' parts, one each
+  const int k = threadIdx.x & 15;
+  RowStat p = {-INFINITY, 0.f, 0.f};
+  if (k < NW) p = RowStat{lds[3 * k], lds[3 * k + 1], ENT ? lds[3 * k + 2] : 0.f};
+  RowStat all = rebase<ENT>(p, lanes_max<16>(p.mx), c);
+  all.s = lanes_sum<16>(all.s);
+  if (ENT) all.sd = lanes_sum<16>(all.sd);
   return all;
   }
 }
@@ -109,6 +106,9 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
 // ---- 16 bytes of a row
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
+// From here on the compiler knows nothing of a piece's value, so that it unpacks it again in the next pass over the row instead of
+// keeping all of it in 32 bits (which needs two to four times the registers).
+__device__ __forceinline__ void forget(u32x4_t& v) { asm volatile("" : "+v"(v)); }
 template <class T> struct Piece { static constexpr int N = 16 / sizeof(T); };
 template <class T> __device__ __forceinline__ u32x4_t load_piece(const T* p) { return *reinterpret_cast<const u32x4_any_t*>(p); }
 template <class T> __device__ __forceinline__ void store_piece(T* p, u32x4_t v) { *reinterpret_cast<u32x4_any_t*>(p) = v; }
@@ -422,11 +422,11 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_loss(RowArgs a) {
   asm volatile("" : "+v"(xt));   // read before the barrier: the gradient may lie in the logits' memory
   float m = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < K; ++k) m = fmaxf(m, max_piece<T>(v[k]));
+  for (int k = 0; k < K; ++k) { m = fmaxf(m, max_piece<T>(v[k])); forget(v[k]); }
   RowStat r = {lanes_max<G < 64 ? G : 64>(m), 0.f, 0.f};
   const float base = r.base();
 #pragma unroll
-  for (int k = 0; k < K; ++k) add_piece<T, ENT>(r, v[k], base, c);
+  for (int k = 0; k < K; ++k) { add_piece<T, ENT>(r, v[k], base, c); forget(v[k]); }
   r = group_join<G, ENT>(r, c, lds);
   if (r.idle()) {
     zero_row(y, a.vocab, tid, G);
