@@ -4,6 +4,9 @@
 // output number c / 4 holds four 16-bit fields, and column c is kept when field c % 4 is at least q = round(65536 p).
 // So y = keep ? x * 65536 / (65536 - q) : 0, plus the residual, in fp32, rounded once to the tensors' type.  The backward
 // pass is the same call on the gradient.
+//
+// Bound by memory: an output serves four columns (fp32) or two outputs eight (16 bits), about 15 vector instructions a column
+// where the time of its bytes holds 35; the hash of (seed, layer) is made on the host, that of the row id once per thread.
 #pragma once
 #include "elem.hip.h"
 #include "splitmix.hip.h"
@@ -13,25 +16,47 @@ struct DropoutArgs {
   const void *x, *residual;  // residual: may be NULL
   void* y;
   const int64_t* ids;        // NULL: a row's id is its number
-  uint64_t seed, layer;
+  uint64_t prefix;           // hash of (seed, layer)
   uint32_t border;           // q
   float scale;
 };
 
-template <class T>
+// A group of G threads does a slice of G DROP_PIECES pieces of a row: blockIdx.x the slice (G < 256: the row is one slice),
+// blockIdx.y and z the row.
+constexpr int DROP_PIECES = 4;
+template <class T, int G, bool RES>
 __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
-  const int64_t groups = (a.cols + 3) / 4, n = a.rows * groups;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / groups, g = i - row * groups;
-    const uint64_t state = perm_stream(a.seed, a.layer, a.ids ? (uint64_t)a.ids[row] : (uint64_t)row);
-    const uint64_t z = sm64_mix(state + (uint64_t)(g + 1) * 0x9E3779B97F4A7C15ULL);
-    for (int k = 0; k < 4; ++k) {
-      const int64_t c = 4 * g + k;
-      if (c >= a.cols) break;
-      const bool keep = ((uint32_t)(z >> (16 * k)) & 0xffffu) >= a.border;
-      float y = keep ? to_f(((const T*)a.x)[row * a.ldx + c]) * a.scale : 0.f;
-      if (a.residual) y += to_f(((const T*)a.residual)[row * a.ldr + c]);
-      ((T*)a.y)[row * a.ldy + c] = from_f<T>(y);
+  constexpr int N = Piece<T>::N;
+  const int64_t row = G < 256 ? (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G : blockIdx.y + (int64_t)blockIdx.z * 65535;
+  if (row >= a.rows) return;
+  const int n = (int)a.cols, from = (G < 256 ? 0 : blockIdx.x * (G * DROP_PIECES * N)) + threadIdx.x % G * N;
+  const T *x = (const T*)a.x + row * a.ldx, *r = RES ? (const T*)a.residual + row * a.ldr : nullptr;
+  T* y = (T*)a.y + row * a.ldy;
+  u32x4_t v[DROP_PIECES], w[DROP_PIECES];
+#pragma unroll
+  for (int u = 0; u < DROP_PIECES; ++u) {
+    v[u] = load_row(x, from + u * G * N, n);
+    if (RES) w[u] = load_row(r, from + u * G * N, n);
+  }
+  const uint64_t G64 = 0x9E3779B97F4A7C15ULL;
+  const uint64_t state = sm64_mix(a.prefix ^ ((a.ids ? (uint64_t)a.ids[row] : (uint64_t)row) + G64));
+#pragma unroll
+  for (int u = 0; u < DROP_PIECES; ++u) {
+    const int at = from + u * G * N;
+    if (at >= n) break;
+    float f[N], g[N];
+    unpack(v[u], f, T());
+    if (RES) unpack(w[u], g, T());
+#pragma unroll
+    for (int h = 0; h < N; h += 4) {
+      const uint64_t z = sm64_mix(state + (uint64_t)(at / 4 + h / 4 + 1) * G64);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t half = (uint32_t)(z >> (k & 2 ? 32 : 0)), field = k & 1 ? half >> 16 : half & 0xffffu;
+        const float kept = field >= a.border ? f[h + k] * a.scale : 0.f;
+        f[h + k] = RES ? kept + g[h + k] : kept;
+      }
     }
+    store_row(y, at, n, pack(f, T()));
   }
 }

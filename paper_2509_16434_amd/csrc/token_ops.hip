@@ -91,6 +91,15 @@ void with_type(int32_t dtype, F f) {
   else if (dtype == 1) f(bf16_t());
   else f(f16_t());
 }
+// Groups of threads per sequence of the preference loss: enough that few long sequences fill the chip, none with less than 1024 tokens
+// on the average.
+int pair_slices(int64_t pairs, int64_t tokens) {
+  if (pairs == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({cdiv(2048, 2 * pairs), tokens / (2 * pairs) / 1024, 256}));
+}
+
+int64_t gae_tiles(int64_t tokens) { return cdiv(tokens, GAE_TILE); }
+
 template <class F>
 void with_flag(bool on, F f) {
   if (on) f(std::true_type());
@@ -140,10 +149,22 @@ int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int6
   if (d_residual) CHECK(check_rows("d_residual", d_residual, dtype, cols, ld_residual));
   CHECK(check_array("d_row_ids", d_row_ids, 8, false));
   const uint32_t border = (uint32_t)(p * 65536 + 0.5);
-  const DropoutArgs a = {rows, cols, ld_x, ld_residual, ld_y, d_x, d_residual, d_y, d_row_ids, seed, layer, border,
+  const uint64_t G64 = 0x9E3779B97F4A7C15ULL;
+  const uint64_t prefix = sm64_mix(sm64_mix(seed + G64) ^ (layer + G64));   // the first two steps of perm_stream
+  const DropoutArgs a = {rows, cols, ld_x, ld_residual, ld_y, d_x, d_residual, d_y, d_row_ids, prefix, border,
                          border < 65536 ? 65536.f / (float)(65536 - border) : 0.f};
-  const int grid = (int)std::min<int64_t>(cdiv(rows * cdiv(cols, 4), 256), 1 << 20);
-  with_type(dtype, [&](auto t) { hipLaunchKernelGGL(k_dropout<decltype(t)>, dim3(grid), dim3(256), 0, (hipStream_t)hip_stream, a); });
+  hipStream_t st = (hipStream_t)hip_stream;
+  with_type(dtype, [&](auto t) {
+    with_flag(d_residual != nullptr, [&](auto res) {
+      using T = decltype(t);
+      constexpr bool RES = decltype(res)::value;
+      const int64_t pieces = cdiv(cols, Piece<T>::N);
+      if (pieces <= 16 * DROP_PIECES) hipLaunchKernelGGL((k_dropout<T, 16, RES>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
+      else if (pieces <= 64 * DROP_PIECES) hipLaunchKernelGGL((k_dropout<T, 64, RES>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
+      else hipLaunchKernelGGL((k_dropout<T, 256, RES>), dim3((uint32_t)cdiv(pieces, 256 * DROP_PIECES), (uint32_t)std::min<int64_t>(rows, 65535), (uint32_t)cdiv(rows, 65535)),
+                              dim3(256), 0, st, a);
+    });
+  });
   LAUNCHCHK("k_dropout");
   return PPO_OK;
 }
@@ -263,7 +284,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
 
 int64_t ppo_pair_ws_bytes(int64_t pairs, int64_t tokens) {
   if (pairs < 0 || pairs > MAX_ROWS / 2 || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
-  return pairs * (int64_t)sizeof(PairRecord);
+  return pairs * (int64_t)sizeof(PairRecord) + 2 * pairs * pair_slices(pairs, tokens) * (int64_t)sizeof(double2);
 }
 
 int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const float* d_logp_ref, const uint8_t* d_mask, const int64_t* d_offsets,
@@ -282,10 +303,18 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
   CHECK(check_array("d_offsets", d_offsets, 8, pairs > 0 || tokens > 0));
   CHECK(check_ws(d_ws, ws_bytes, ppo_pair_ws_bytes(pairs, tokens)));
   const PairArgs a = {pairs, tokens, d_logp, d_logp_ref, d_mask, d_offsets, hp->kind, hp->length_mean, hp->beta, hp->label_smoothing, hp->scale,
-                      d_dlogp, d_margin, d_stats, (PairRecord*)d_ws};
+                      d_dlogp, d_margin, (PairRecord*)d_ws};
   hipStream_t st = (hipStream_t)hip_stream;
-  if (pairs > 0) hipLaunchKernelGGL(k_pair_loss, dim3((uint32_t)pairs), dim3(256), 0, st, a);
-  if (tokens > 0) hipLaunchKernelGGL(k_pair_outside, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 65536)), dim3(256), 0, st, a);
+  const PairGrid g = {pair_slices(pairs, tokens), (double2*)(a.record + pairs)};
+  const int64_t items = 2 * pairs * g.slices;
+  if (pairs == 0 && tokens > 0) hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 1024)), dim3(256), 0, st, a, g);
+  else if (pairs > 0 && tokens / (2 * pairs) <= 512) {
+    hipLaunchKernelGGL(k_pair_sums<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL(k_pair_loss<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
+  } else if (pairs > 0) {
+    hipLaunchKernelGGL(k_pair_sums<256>, dim3((uint32_t)items), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)items), dim3(256), 0, st, a, g);
+  }
   hipLaunchKernelGGL(k_pair_stats, dim3(1), dim3(1024), 0, st, pairs, (const PairRecord*)d_ws, hp->scale, d_stats);
   LAUNCHCHK("the kernels of ppo_pair_loss");
   return PPO_OK;
@@ -293,7 +322,8 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
 
 int64_t ppo_token_gae_ws_bytes(int64_t sequences, int64_t tokens) {
   if (sequences < 0 || sequences > MAX_ROWS || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
-  return 0;
+  const int64_t tiles = gae_tiles(tokens);
+  return tiles <= 1 ? 0 : tiles * (int64_t)sizeof(GaeMap) + (tiles > GAE_DIRECT ? tiles * (int64_t)sizeof(double2) : 0);
 }
 
 int ppo_token_gae(int64_t sequences, int64_t tokens, const float* d_reward, const float* d_value, const uint8_t* d_mask, const int64_t* d_offsets,
@@ -308,10 +338,15 @@ int ppo_token_gae(int64_t sequences, int64_t tokens, const float* d_reward, cons
   CHECK(check_array("d_adv", d_adv, 4, true));
   CHECK(check_array("d_ret", d_ret, 4, true));
   CHECK(check_ws(d_ws, ws_bytes, ppo_token_gae_ws_bytes(sequences, tokens)));
-  const GaeArgs a = {sequences, tokens, d_reward, d_value, d_last_value, d_mask, d_offsets, gamma, lambda, d_adv, d_ret};
+  const int64_t tiles = gae_tiles(tokens);
+  GaeMap* map = tiles > 1 ? (GaeMap*)d_ws : nullptr;
+  double2* in = tiles > GAE_DIRECT ? (double2*)d_ws : nullptr;
+  if (in) map = (GaeMap*)(in + tiles);
+  const GaeArgs a = {sequences, tokens, d_reward, d_value, d_last_value, d_mask, d_offsets, gamma, lambda, d_adv, d_ret, tiles, map, in};
   hipStream_t st = (hipStream_t)hip_stream;
-  hipLaunchKernelGGL(k_gae_outside, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 65536)), dim3(256), 0, st, a);
-  if (sequences > 0) hipLaunchKernelGGL(k_token_gae, dim3((uint32_t)sequences), dim3(64), 0, st, a);
+  if (tiles > 1) hipLaunchKernelGGL(k_gae_part, dim3((uint32_t)tiles), dim3(256), 0, st, a);
+  if (in) hipLaunchKernelGGL(k_gae_tiles, dim3(1), dim3(1024), 0, st, a);
+  hipLaunchKernelGGL(k_token_gae, dim3((uint32_t)tiles), dim3(256), 0, st, a);
   LAUNCHCHK("the kernels of ppo_token_gae");
   return PPO_OK;
 }
