@@ -248,7 +248,8 @@ int ppo_forward(ppo_ctx* ctx, const int32_t* d_idx, int64_t count, float* d_mu, 
  * every call may be recorded into a graph.  d_ws is scratch of at least the bytes that the *_ws_bytes function gives
  * for the same sizes, 16-byte aligned; nothing is kept in it between calls, and two calls whose work may overlap in time
  * need two of them (so do two captured graphs that may).  Errors are reported through ppo_last_error(NULL); arguments are
- * checked before any HIP call.  Results are the same, bit for bit, every time.  An empty call (no rows, tokens or
+ * checked before any HIP call.  The same call gives the same results, bit for bit, every time (the order in which a row is added
+ * up goes by its length, its alignment and the number of rows).  An empty call (no rows, tokens or
  * sequences) is allowed; the array pointers that it would read may then be NULL.
  *
  * `dtype` is the type of the large arrays: 0 fp32, 1 bf16, 2 fp16; everything else is fp32 or as declared, and every sum

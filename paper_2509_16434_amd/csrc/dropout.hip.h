@@ -32,18 +32,20 @@ __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
   const int n = (int)a.cols, from = (G < 256 ? 0 : blockIdx.x * (G * DROP_PIECES * N)) + threadIdx.x % G * N;
   const T *x = (const T*)a.x + row * a.ldx, *r = RES ? (const T*)a.residual + row * a.ldr : nullptr;
   T* y = (T*)a.y + row * a.ldy;
+  const int full = n & ~(N - 1), tid = threadIdx.x % G;   // the last n % N columns are taken one by one
+  const uint64_t G64 = 0x9E3779B97F4A7C15ULL;
   u32x4_t v[DROP_PIECES], w[DROP_PIECES];
 #pragma unroll
-  for (int u = 0; u < DROP_PIECES; ++u) {
-    v[u] = load_row(x, from + u * G * N, n);
-    if (RES) w[u] = load_row(r, from + u * G * N, n);
-  }
-  const uint64_t G64 = 0x9E3779B97F4A7C15ULL;
+  for (int u = 0; u < DROP_PIECES; ++u)
+    if (from + u * G * N < full) {
+      v[u] = load_piece(x + from + u * G * N);
+      if (RES) w[u] = load_piece(r + from + u * G * N);
+    }
   const uint64_t state = sm64_mix(a.prefix ^ ((a.ids ? (uint64_t)a.ids[row] : (uint64_t)row) + G64));
 #pragma unroll
   for (int u = 0; u < DROP_PIECES; ++u) {
     const int at = from + u * G * N;
-    if (at >= n) break;
+    if (at >= full) break;
     float f[N], g[N];
     unpack(v[u], f, T());
     if (RES) unpack(w[u], g, T());
@@ -57,6 +59,12 @@ __global__ __launch_bounds__(256) void k_dropout(DropoutArgs a) {
         f[h + k] = RES ? kept + g[h + k] : kept;
       }
     }
-    store_row(y, at, n, pack(f, T()));
+    store_piece(y + at, pack(f, T()));
+  }
+  if ((G < 256 || blockIdx.x == 0) && tid < n - full) {
+    const int c = full + tid;
+    const uint64_t z = sm64_mix(state + (uint64_t)(c / 4 + 1) * G64);
+    const float kept = ((uint32_t)(z >> (c % 4 * 16)) & 0xffffu) >= a.border ? to_f(x[c]) * a.scale : 0.f;
+    y[c] = from_f<T>(RES ? kept + to_f(r[c]) : kept);
   }
 }

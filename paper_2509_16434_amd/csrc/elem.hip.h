@@ -55,39 +55,21 @@ __device__ __forceinline__ u32x4_t pack(const float (&f)[8], f16_t) {
   for (int i = 0; i < 4; ++i) { const h2_t h = {(_Float16)f[2 * i], (_Float16)f[2 * i + 1]}; v[i] = __builtin_bit_cast(uint32_t, h); }
   return v;
 }
-// two lowest-valued logits, for the places behind the end of a row
-__device__ __forceinline__ uint32_t no_logits(float) { return 0xff800000u; }
-__device__ __forceinline__ uint32_t no_logits(bf16_t) { return 0xff80ff80u; }
-__device__ __forceinline__ uint32_t no_logits(f16_t) { return 0xfc00fc00u; }
-// elements i .. i + N - 1 of a row (or part) of n elements; those behind its end are -infinity
-template <class T>
-__device__ __forceinline__ u32x4_t load_row(const T* x, int i, int n) {
+// A row of n elements at x, as a group of threads takes it: `head` elements up to the first 16-byte boundary, `full` elements in
+// whole pieces from there, and a tail.  Head and tail (fewer than N elements each) are taken one by one, by the threads 0 .. and
+// 8 .. : `one` is this thread's place among them, or -1.  Pieces across the boundaries of cache lines cost a sixth of the rate.
+struct Cut { int head, full, one; };
+template <class T> __device__ __forceinline__ Cut cut_row(const T* x, int n, int tid) {
   constexpr int N = Piece<T>::N;
-  const uint32_t none = no_logits(T());
-  u32x4_t v = {none, none, none, none};
-  if (i + N <= n) v = load_piece(x + i);
-  else if (i < n) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (i + k < n) {
-        if constexpr (sizeof(T) == 4) v[k] = __float_as_uint(x[i + k]);
-        else { const T one = x[i + k]; const uint32_t h = __builtin_bit_cast(uint16_t, one); v[k >> 1] = k & 1 ? (v[k >> 1] & 0xffffu) | (h << 16) : (v[k >> 1] & 0xffff0000u) | h; }
-      }
-    }
-  }
-  return v;
+  Cut c;
+  c.head = min(n, (int)((0u - (uint32_t)((uintptr_t)x / sizeof(T))) & (N - 1)));
+  c.full = (n - c.head) & ~(N - 1);
+  const int tail = n - c.head - c.full;
+  c.one = tid < c.head ? tid : tid >= 8 && tid - 8 < tail ? c.head + c.full + tid - 8 : -1;
+  return c;
 }
-template <class T>
-__device__ __forceinline__ void store_row(T* y, int i, int n, u32x4_t v) {
-  constexpr int N = Piece<T>::N;
-  if (i + N <= n) store_piece(y + i, v);
-  else if (i < n) {
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-      if (i + k < n) {
-        if constexpr (sizeof(T) == 4) y[i + k] = __uint_as_float(v[k]);
-        else { const uint16_t h = (uint16_t)(v[k >> 1] >> (k & 1 ? 16 : 0)); y[i + k] = __builtin_bit_cast(T, h); }
-      }
-    }
-  }
+// whether a group's thread tid writes element t of the row (G threads, its pieces G apart)
+template <class T, int G> __device__ __forceinline__ bool owns(const Cut& c, int t, int tid) {
+  const int r = t - c.head;
+  return r >= 0 && r < c.full ? r / Piece<T>::N % G == tid : t == c.one;
 }

@@ -84,6 +84,13 @@ void set_slices(RowArgs& a) {
   a.slices = (int32_t)cdiv(a.vocab, a.slice_len);
 }
 
+// Workspace of a call on rows: parts of the slices (16 bytes each), records of the loss, then sums of the blocks that add those up.
+int stats_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, STATS_ROWS), 1024)); }
+int64_t stats_offset(int64_t rows, int64_t vocab) {
+  const int s = slices_of(std::max<int64_t>(rows, 1), vocab);
+  return ((s > 1 ? rows * s * 16 : 0) + rows * (int64_t)sizeof(LossRecord) + 15) / 16 * 16;
+}
+
 // f(element type) for the type named by dtype
 template <class F>
 void with_type(int32_t dtype, F f) {
@@ -171,8 +178,7 @@ int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int6
 
 int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab) {
   if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return PPO_ESHAPE;
-  const int s = slices_of(std::max<int64_t>(rows, 1), vocab);
-  return (s > 1 ? rows * s * 16 : 0) + rows * (int64_t)sizeof(LossRecord);
+  return stats_offset(rows, vocab) + (stats_blocks(rows) > 1 ? stats_blocks(rows) * 48 : 0);
 }
 
 int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, float temperature, float* d_logp,
@@ -277,7 +283,10 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
     });
     LAUNCHCHK("k_token_loss");
   }
-  hipLaunchKernelGGL(k_token_stats, dim3(1), dim3(1024), 0, st, rows, (const LossRecord*)a.record, hp->kl_coef, hp->ent_coef, d_stats);
+  const int blocks = stats_blocks(rows);
+  double* part = (double*)((char*)d_ws + stats_offset(rows, vocab));
+  hipLaunchKernelGGL(k_token_stats, dim3(blocks), dim3(1024), 0, st, rows, cdiv(std::max<int64_t>(rows, 1), blocks), (const LossRecord*)a.record, hp->kl_coef, hp->ent_coef, d_stats, part);
+  if (blocks > 1) hipLaunchKernelGGL(k_token_stats_join, dim3(1), dim3(1024), 0, st, blocks, hp->kl_coef, hp->ent_coef, d_stats, (const double*)part);
   LAUNCHCHK("k_token_stats");
   return PPO_OK;
 }
@@ -308,7 +317,7 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
   const PairGrid g = {pair_slices(pairs, tokens), (double2*)(a.record + pairs)};
   const int64_t items = 2 * pairs * g.slices;
   if (pairs == 0 && tokens > 0) hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 1024)), dim3(256), 0, st, a, g);
-  else if (pairs > 0 && tokens / (2 * pairs) <= 512) {
+  else if (pairs > 0 && (tokens / (2 * pairs) <= 64 || (pairs >= 2048 && tokens / (2 * pairs) <= 512))) {
     hipLaunchKernelGGL(k_pair_sums<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
     hipLaunchKernelGGL(k_pair_loss<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
   } else if (pairs > 0) {

@@ -12,6 +12,7 @@
 // hold 16-byte pieces of it; rows of any alignment are read and written in such pieces (the hardware takes them at any address).
 #pragma once
 #include "elem.hip.h"
+#include "lanes.hip.h"
 
 struct RowArgs {
   int64_t rows, ld, ldd;   // row strides of the logits and of their gradient
@@ -45,27 +46,6 @@ struct RowStat {
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }  // 1 ulp; results below 2^-126 are 0
 // d of a logit of -infinity is -infinity: as a factor it is held at a finite value, so that 0 * d stays 0
 __device__ __forceinline__ float finite_d(float d) { return fmaxf(d, -1e30f); }
-
-// ---- over the lanes of a wave: within 16 lanes by permutations of the operand, then across
-template <int CTRL> __device__ __forceinline__ float dpp(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
-}
-#define DPP_XOR1 0xB1         // quad_perm [1,0,3,2]
-#define DPP_XOR2 0x4E         // quad_perm [2,3,0,1]
-#define DPP_HALF_MIRROR 0x141
-#define DPP_MIRROR 0x140
-// over groups of W = 16 or 64 lanes
-template <int W> __device__ __forceinline__ float lanes_max(float v) {
-  v = fmaxf(v, dpp<DPP_XOR1>(v)); v = fmaxf(v, dpp<DPP_XOR2>(v));
-  v = fmaxf(v, dpp<DPP_HALF_MIRROR>(v)); v = fmaxf(v, dpp<DPP_MIRROR>(v));
-  if (W == 64) { v = fmaxf(v, __shfl_xor(v, 16)); v = fmaxf(v, __shfl_xor(v, 32)); }
-  return v;
-}
-template <int W> __device__ __forceinline__ float lanes_sum(float v) {
-  v += dpp<DPP_XOR1>(v); v += dpp<DPP_XOR2>(v); v += dpp<DPP_HALF_MIRROR>(v); v += dpp<DPP_MIRROR>(v);
-  if (W == 64) { v += __shfl_xor(v, 16); v += __shfl_xor(v, 32); }
-  return v;
-}
 
 // ---- statistics of parts of a row, joined
 // b's sums with respect to the maximum mx (>= b.mx)
@@ -103,17 +83,19 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
   }
 }
 
-// adds a piece's terms to r, whose maximum covers them
+// adds an element's, a piece's terms to r, whose maximum covers them
+template <bool ENT>
+__device__ __forceinline__ void add_one(RowStat& r, float x, float base, float c) {
+  const float d = x - base, e = exp2_hw(d * c);
+  r.s += e;
+  if (ENT) r.sd += e * finite_d(d);
+}
 template <class T, bool ENT>
 __device__ __forceinline__ void add_piece(RowStat& r, u32x4_t v, float base, float c) {
   float f[Piece<T>::N];
   unpack(v, f, T());
 #pragma unroll
-  for (int k = 0; k < Piece<T>::N; ++k) {
-    const float d = f[k] - base, e = exp2_hw(d * c);
-    r.s += e;
-    if (ENT) r.sd += e * finite_d(d);
-  }
+  for (int k = 0; k < Piece<T>::N; ++k) add_one<ENT>(r, f[k], base, c);
 }
 template <class T>
 __device__ __forceinline__ float max_piece(u32x4_t v) {
@@ -130,18 +112,25 @@ __device__ __forceinline__ float max_piece(u32x4_t v) {
 template <class T, int G, bool ENT>
 __device__ __forceinline__ RowStat stream_stat(const T* x, int n, int tid, float c) {
   constexpr int N = Piece<T>::N, U = 4;
-  RowStat r = {-INFINITY, 0.f, 0.f};
-  for (int i = tid * N; i < n; i += G * N * U) {
+  const Cut q = cut_row(x, n, tid);
+  RowStat r = {q.one >= 0 ? to_f(x[q.one]) : -INFINITY, 0.f, 0.f};
+  if (r.mx > -INFINITY) r.s = 1.f;
+  else if (r.mx != r.mx) r = RowStat{-INFINITY, NAN, NAN};
+  x += q.head;
+  for (int i = tid * N; i < q.full; i += G * N * U) {
     u32x4_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, n);
     float m = r.mx;
 #pragma unroll
-    for (int u = 0; u < U; ++u) m = fmaxf(m, max_piece<T>(v[u]));
+    for (int u = 0; u < U; ++u)
+      if (i + u * G * N < q.full) v[u] = load_piece(x + i + u * G * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * G * N < q.full) m = fmaxf(m, max_piece<T>(v[u]));
     r = rebase<ENT>(r, m, c);
     const float base = r.base();
 #pragma unroll
-    for (int u = 0; u < U; ++u) add_piece<T, ENT>(r, v[u], base, c);
+    for (int u = 0; u < U; ++u)
+      if (i + u * G * N < q.full) add_piece<T, ENT>(r, v[u], base, c);
   }
   return r;
 }
@@ -222,54 +211,66 @@ struct GradCoef { float mx, c, k0, k1, add; };
 __device__ __forceinline__ GradCoef grad_coef(float g, float h, float ent, float ls, float mx, float is, float inv_t) {
   return GradCoef{mx, inv_t * TOKEN_LOG2E, (g + h * (ent - ls)) * is, h * inv_t * is, g * inv_t};
 }
-// t: the target's place in the piece, if it is in it
+template <bool ENT>
+__device__ __forceinline__ float grad_one(float x, const GradCoef& k) {
+  const float d = x - k.mx, e = exp2_hw(d * k.c);
+  return -e * (ENT ? k.k0 + k.k1 * finite_d(d) : k.k0);
+}
 template <class T, bool ENT>
-__device__ __forceinline__ u32x4_t grad_piece(u32x4_t v, const GradCoef& k, int t) {
+__device__ __forceinline__ u32x4_t grad_piece(u32x4_t v, const GradCoef& k) {
   constexpr int N = Piece<T>::N;
   float f[N];
   unpack(v, f, T());
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const float d = f[i] - k.mx, e = exp2_hw(d * k.c);
-    f[i] = -e * (ENT ? k.k0 + k.k1 * finite_d(d) : k.k0);
-  }
-  if ((unsigned)t < (unsigned)N) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) f[i] += i == t ? k.add : 0.f;
-  }
+  for (int i = 0; i < N; ++i) f[i] = grad_one<ENT>(f[i], k);
   return pack(f, T());
 }
 template <class T>
 __device__ __forceinline__ void zero_row(T* y, int n, int tid, int G) {
   const u32x4_t z = {0, 0, 0, 0};
-  for (int i = tid * Piece<T>::N; i < n; i += G * Piece<T>::N) store_row(y, i, n, z);
+  const Cut q = cut_row(y, n, tid);
+  for (int i = tid * Piece<T>::N; i < q.full; i += G * Piece<T>::N) store_piece(y + q.head + i, z);
+  if (q.one >= 0) y[q.one] = from_f<T>(0.f);
 }
 
 // Gradient of the log-probability and the entropy from the row's statistics: every piece by itself.  A group of G threads does a
 // slice of G BACK_PIECES pieces of a row: blockIdx.x the slice (G < 256: the row is one slice), blockIdx.y and z the row.
-constexpr int BACK_PIECES = 4;
+constexpr int BACK_PIECES = 4;   // pieces per thread
 template <class T, int G, bool ENT>
 __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
   constexpr int N = Piece<T>::N;
   const int64_t row = G < 256 ? (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G : blockIdx.y + (int64_t)blockIdx.z * 65535;
   if (row >= a.rows) return;
   const int t = a.target[row], from = (G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N)) + threadIdx.x % G * N;
+  const int tid = threadIdx.x % G;
   const T* x = (const T*)a.logits + row * a.ld;
   T* y = (T*)a.dlogits + row * a.ldd;
+  Cut q = cut_row(x, a.vocab, tid);
+  if (G >= 256 && blockIdx.x) q.one = -1;   // the first slice's threads take head and tail
   const float mx = a.stat[2 * row], ls = a.stat[2 * row + 1];
-  const u32x4_t z = {0, 0, 0, 0};
   if (t < 0 || t >= a.vocab || mx == -INFINITY) {
+    const u32x4_t z = {0, 0, 0, 0};
 #pragma unroll
-    for (int u = 0; u < BACK_PIECES; ++u) store_row(y, from + u * G * N, a.vocab, z);
+    for (int u = 0; u < BACK_PIECES; ++u)
+      if (from + u * G * N < q.full) store_piece(y + q.head + from + u * G * N, z);
+    if (q.one >= 0) y[q.one] = from_f<T>(0.f);
     return;
   }
   const float g = a.dlogp[row], h = ENT ? a.dentropy[row] : 0.f, H = ENT ? a.entropy[row] : 0.f;
   const GradCoef k = grad_coef(g, h, H, ls, mx, expf(-ls) * a.inv_t, a.inv_t);
+  // the target's element is written again, by the thread that wrote it
+  const int slice = G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N), r = t - q.head;
+  const bool owner = r >= 0 && r < q.full ? r >= slice && r < slice + G * BACK_PIECES * N && (r - slice) / N % G == tid : t == q.one;
+  const float xt = owner ? to_f(x[t]) : 0.f, xl = q.one >= 0 ? to_f(x[q.one]) : 0.f;
   u32x4_t v[BACK_PIECES];
 #pragma unroll
-  for (int u = 0; u < BACK_PIECES; ++u) v[u] = load_row(x, from + u * G * N, a.vocab);
+  for (int u = 0; u < BACK_PIECES; ++u)
+    if (from + u * G * N < q.full) v[u] = load_piece(x + q.head + from + u * G * N);
 #pragma unroll
-  for (int u = 0; u < BACK_PIECES; ++u) store_row(y, from + u * G * N, a.vocab, grad_piece<T, ENT>(v[u], k, t - (from + u * G * N)));
+  for (int u = 0; u < BACK_PIECES; ++u)
+    if (from + u * G * N < q.full) store_piece(y + q.head + from + u * G * N, grad_piece<T, ENT>(v[u], k));
+  if (q.one >= 0) y[q.one] = from_f<T>(grad_one<ENT>(xl, k));
+  if (owner) y[t] = from_f<T>(grad_one<ENT>(xt, k) + k.add);
 }
 
 // ---- loss
@@ -318,7 +319,7 @@ __device__ __forceinline__ void loss_idle(const RowArgs& a, int64_t row) {
 // Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers between the pass that
 // adds up and the one that writes, so that memory sees it once in and once out.
 template <class T, int G, int K, bool ENT>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_loss(RowArgs a) {
+__global__ __launch_bounds__(G < 256 ? 256 : G, K == 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
   constexpr int NT = G < 256 ? 256 : G, N = Piece<T>::N;
   __shared__ float lds[3 * (NT / 64)];
   const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);
@@ -334,17 +335,24 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_loss(RowArgs a) {
   const float c = a.inv_t * TOKEN_LOG2E;
   const LossIn in = loss_in(a, row);
   float xt = to_f(x[t]);
+  const Cut w = cut_row(x, a.vocab, tid);
+  const int full = w.full;
+  const float xl = w.one >= 0 ? to_f(x[w.one]) : -INFINITY;
   u32x4_t v[K];
 #pragma unroll
-  for (int k = 0; k < K; ++k) v[k] = load_row(x, at + k * G * N, a.vocab);
+  for (int k = 0; k < K; ++k)
+    if (at + k * G * N < full) v[k] = load_piece(x + w.head + at + k * G * N);
   asm volatile("" : "+v"(xt));   // read before the barrier: the gradient may lie in the logits' memory
-  float m = -INFINITY;
+  float m = xl;
 #pragma unroll
-  for (int k = 0; k < K; ++k) { m = fmaxf(m, max_piece<T>(v[k])); forget(v[k]); }
+  for (int k = 0; k < K; ++k)
+    if (at + k * G * N < full) { m = fmaxf(m, max_piece<T>(v[k])); forget(v[k]); }
   RowStat r = {lanes_max<G < 64 ? G : 64>(m), 0.f, 0.f};
   const float base = r.base();
 #pragma unroll
-  for (int k = 0; k < K; ++k) { add_piece<T, ENT>(r, v[k], base, c); forget(v[k]); }
+  for (int k = 0; k < K; ++k)
+    if (at + k * G * N < full) { add_piece<T, ENT>(r, v[k], base, c); forget(v[k]); }
+  if (w.one >= 0) add_one<ENT>(r, xl, base, c);
   r = group_join<G, ENT>(r, c, lds);
   if (r.idle()) {
     zero_row(y, a.vocab, tid, G);
@@ -353,13 +361,36 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_loss(RowArgs a) {
   }
   const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
 #pragma unroll
-  for (int k = 0; k < K; ++k) store_row(y, at + k * G * N, a.vocab, grad_piece<T, ENT>(v[k], q, t - (at + k * G * N)));
+  for (int k = 0; k < K; ++k)
+    if (at + k * G * N < full) store_piece(y + w.head + at + k * G * N, grad_piece<T, ENT>(v[k], q));
+  if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
+  // the target's element again, by the thread that wrote it with its piece
+  if (owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
+}
+
+// The gradient of n elements by G threads; t: the target's place among them, if it is one of them.
+template <class T, int G, bool ENT>
+__device__ __forceinline__ void stream_gradient(const T* x, T* y, int n, int tid, const GradCoef& q, int t, float xt) {
+  constexpr int N = Piece<T>::N, U = 4;
+  const Cut w = cut_row(x, n, tid);
+  const float xl = w.one >= 0 ? to_f(x[w.one]) : 0.f;
+  for (int i = tid * N; i < w.full; i += G * N * U) {
+    u32x4_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * G * N < w.full) v[u] = load_piece(x + w.head + i + u * G * N);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u * G * N < w.full) store_piece(y + w.head + i + u * G * N, grad_piece<T, ENT>(v[u], q));
+  }
+  if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
+  if (t >= 0 && t < n && owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
 }
 
 // Longer rows: read twice by a block.
 template <class T, bool ENT>
 __global__ __launch_bounds__(1024) void k_token_loss_long(RowArgs a) {
-  constexpr int N = Piece<T>::N, G = 1024, U = 4;
+  constexpr int G = 1024;
   __shared__ float lds[3 * (G / 64)];
   const int64_t row = blockIdx.x;
   const int t = a.target[row], tid = threadIdx.x;
@@ -381,20 +412,13 @@ __global__ __launch_bounds__(1024) void k_token_loss_long(RowArgs a) {
     return;
   }
   const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
-  for (int i = tid * N; i < a.vocab; i += G * N * U) {
-    u32x4_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, a.vocab);
-#pragma unroll
-    for (int u = 0; u < U; ++u) store_row(y, i + u * G * N, a.vocab, grad_piece<T, ENT>(v[u], q, t - (i + u * G * N)));
-  }
+  stream_gradient<T, G, ENT>(x, y, a.vocab, tid, q, t, xt);
 }
 
 // Few long rows: k_token_part has left the statistics of the slices; every slice's block joins them all and writes its gradient.
 // The target's logit may be overwritten by the block that owns it before another has read it: part 0's spare place holds it.
 template <class T, bool ENT>
 __global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
-  constexpr int N = Piece<T>::N, G = 256, U = 4;
   const int64_t row = blockIdx.y;
   const int t = a.target[row], tid = threadIdx.x, from = blockIdx.x * a.slice_len, n = min(a.vocab - from, a.slice_len);
   const T* x = (const T*)a.logits + row * a.ld + from;
@@ -403,38 +427,46 @@ __global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
   RowStat r = {-INFINITY, 0.f, 0.f};
   if (t >= 0 && t < a.vocab) r = join_parts<ENT>(a, row, a.inv_t * TOKEN_LOG2E);
   if (r.idle()) {
-    zero_row(y, n, tid, G);
+    zero_row(y, n, tid, 256);
     if (first) loss_idle(a, row);
     return;
   }
-  const GradCoef q = loss_row(a, row, loss_in(a, row), r, a.part[4 * row * a.slices + 3], ENT, first);
-  for (int i = tid * N; i < n; i += G * N * U) {
-    u32x4_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_row(x, i + u * G * N, n);
-#pragma unroll
-    for (int u = 0; u < U; ++u) store_row(y, i + u * G * N, n, grad_piece<T, ENT>(v[u], q, t - (from + i + u * G * N)));
-  }
+  const float xt = a.part[4 * row * a.slices + 3];
+  const GradCoef q = loss_row(a, row, loss_in(a, row), r, xt, ENT, first);
+  stream_gradient<T, 256, ENT>(x, y, n, tid, q, t - from, xt);
 }
 
-// Statistics of the loss: the rows' records added in a fixed order, in 64 bits.
-// stats: loss, pi, kl, entropy (weighted sums), mean approx_kl, clipped share, active rows, non-finite
-__global__ __launch_bounds__(1024) void k_token_stats(int64_t rows, const LossRecord* rec, float kl_coef, float ent_coef, float* stats) {
-  __shared__ double lds[6][16];
-  double v[6] = {0, 0, 0, 0, 0, 0};
-  for (int64_t i = threadIdx.x; i < rows; i += 1024) {
-    const LossRecord r = rec[i];
-    v[0] += r.pi; v[1] += r.kl; v[2] += r.ent; v[3] += r.old_kl; v[4] += r.clipped; v[5] += r.active;
-  }
-  for (int k = 0; k < 6; ++k) {
-    for (int o = 32; o; o >>= 1) v[k] += __shfl_xor(v[k], o);
-    if ((threadIdx.x & 63) == 0) lds[k][threadIdx.x >> 6] = v[k];
-  }
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (int k = 0; k < 6; ++k) { v[k] = 0; for (int w = 0; w < 16; ++w) v[k] += lds[k][w]; }
+// Statistics of the loss: the rows' records added in a fixed order, in 64 bits; block b takes the rows b n .. of its share.  One
+// block finishes by itself; of several, each leaves its sums for k_token_stats_join.
+constexpr int STATS_ROWS = 4096;   // rows per block (more when there are more than 1024 such blocks)
+__device__ __forceinline__ void write_stats(const double (&v)[6], float kl_coef, float ent_coef, float* stats) {
+  // loss, pi, kl, entropy (weighted sums), mean approx_kl, clipped share, active rows, non-finite
   const double loss = v[0] + (double)kl_coef * v[1] - (double)ent_coef * v[2], n = v[5] > 0 ? v[5] : 1;
   stats[0] = (float)loss; stats[1] = (float)v[0]; stats[2] = (float)v[1]; stats[3] = (float)v[2];
   stats[4] = (float)(v[3] / n); stats[5] = (float)(v[4] / n); stats[6] = (float)v[5];
   stats[7] = isfinite((float)loss) ? 0.f : 1.f;
+}
+__global__ __launch_bounds__(1024) void k_token_stats(int64_t rows, int64_t share, const LossRecord* rec, float kl_coef, float ent_coef, float* stats, double* part) {
+  __shared__ double lds[6 * 16];
+  double v[6] = {0, 0, 0, 0, 0, 0};
+  const int64_t from = blockIdx.x * share, to = from + share < rows ? from + share : rows;
+  for (int64_t i = from + threadIdx.x; i < to; i += 4096) {
+    LossRecord r[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) r[u] = i + u * 1024 < to ? rec[i + u * 1024] : LossRecord{0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) { v[0] += r[u].pi; v[1] += r[u].kl; v[2] += r[u].ent; v[3] += r[u].old_kl; v[4] += r[u].clipped; v[5] += r[u].active; }
+  }
+  block_sums<16>(v, lds);
+  if (threadIdx.x) return;
+  if (gridDim.x == 1) write_stats(v, kl_coef, ent_coef, stats);
+  else
+    for (int k = 0; k < 6; ++k) part[6 * blockIdx.x + k] = v[k];
+}
+__global__ __launch_bounds__(1024) void k_token_stats_join(int blocks, float kl_coef, float ent_coef, float* stats, const double* part) {
+  __shared__ double lds[6 * 16];
+  double v[6];
+  for (int k = 0; k < 6; ++k) v[k] = (int)threadIdx.x < blocks ? part[6 * threadIdx.x + k] : 0.0;
+  block_sums<16>(v, lds);
+  if (threadIdx.x == 0) write_stats(v, kl_coef, ent_coef, stats);
 }

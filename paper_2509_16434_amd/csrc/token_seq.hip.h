@@ -1,7 +1,7 @@
 // Sequences packed one behind the other: sequence k holds the tokens [offsets[k], offsets[k+1]).  Offsets are held inside
 // [0, tokens] before they are used, so that a wrong one cannot reach memory outside the arrays.
 #pragma once
-#include "common.hip.h"
+#include "lanes.hip.h"
 
 __device__ __forceinline__ int64_t hold(int64_t o, int64_t tokens) { return o < 0 ? 0 : o > tokens ? tokens : o; }
 
@@ -21,32 +21,14 @@ struct PairArgs {
 };
 struct PairRecord { double loss, right, margin, chosen, rejected, active; };
 
-// v: the same in every lane of a wave
-__device__ __forceinline__ double block_sum_waves(double v, double* lds) {
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0;
-  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) v += lds[w];
-  __syncthreads();
-  return v;
+// loss of a pair, and its derivative by D
+__device__ __forceinline__ double pair_value(int kind, double beta, double ls, double D) {
+  if (kind != 0) { const double e = D - 0.5 / beta; return e * e; }
+  const double x = beta * D, soft = log1p(exp(-fabs(x)));             // -log sigmoid(|x|)
+  return (1 - ls) * (soft + (x < 0 ? -x : 0)) + ls * (soft + (x > 0 ? x : 0));
 }
-__device__ __forceinline__ double block_sum_d(double v, double* lds) {
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return block_sum_waves(v, lds);
-}
-
-// loss of a pair and its derivative by D
-__device__ __forceinline__ void pair_term(int kind, double beta, double ls, double D, double* loss, double* slope) {
-  if (kind == 0) {
-    const double x = beta * D, soft = log1p(exp(-fabs(x)));             // -log sigmoid(|x|)
-    const double pos = soft + (x < 0 ? -x : 0), neg = soft + (x > 0 ? x : 0);
-    *loss = (1 - ls) * pos + ls * neg;
-    *slope = beta * (ls - 1 / (1 + exp(x)));
-  } else {
-    const double e = D - 0.5 / beta;
-    *loss = e * e;
-    *slope = 2 * e;
-  }
+__device__ __forceinline__ double pair_slope(int kind, double beta, double ls, double D) {
+  return kind != 0 ? 2 * (D - 0.5 / beta) : beta * (ls - 1 / (1 + exp(beta * D)));
 }
 
 // What a launch of the two kernels below knows of the grid: a sequence is worked on by `slices` groups of G threads, four tokens a
@@ -92,7 +74,7 @@ __device__ __forceinline__ void store4(float* p, int64_t i, int64_t to, const fl
 
 template <int G>
 __global__ __launch_bounds__(256) void k_pair_sums(PairArgs a, PairGrid g) {
-  __shared__ double lds[4];
+  __shared__ double lds[8];
   const int64_t item = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;   // a sequence's slice
   if (G == 64 && item >= 2 * a.pairs * g.slices) return;
   const int64_t s = item / g.slices;
@@ -109,21 +91,17 @@ __global__ __launch_bounds__(256) void k_pair_sums(PairArgs a, PairGrid g) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) { v += on[k] ? (double)x[k] - (double)r[k] : 0.0; c += on[k]; }
   }
-  double n = c;
-  for (int o = 32; o; o >>= 1) { v += __shfl_xor(v, o); n += __shfl_xor(n, o); }
-  if (G > 64) {
-    v = block_sum_waves(v, lds);
-    n = block_sum_waves(n, lds);
-  }
-  if (threadIdx.x % G == 0) g.part[item] = make_double2(v, n);
+  double sums[2] = {v, (double)c};
+  block_sums<G / 64>(sums, lds);
+  if (threadIdx.x % G == 0) g.part[item] = make_double2(sums[0], sums[1]);
 }
 
 // S and number of unmasked tokens of a sequence, by every lane of a wave
 __device__ __forceinline__ double2 pair_sum(const PairGrid& g, int64_t s) {
+  if (g.slices == 1) return g.part[s];
   double v = 0, n = 0;
   for (int k = threadIdx.x & 63; k < g.slices; k += 64) { const double2 p = g.part[s * g.slices + k]; v += p.x; n += p.y; }
-  for (int o = 32; o; o >>= 1) { v += __shfl_xor(v, o); n += __shfl_xor(n, o); }
-  return make_double2(v, n);
+  return make_double2(lanes_sum<64>(v), lanes_sum<64>(n));
 }
 
 // Gradient (and record) of the pairs.
@@ -141,9 +119,7 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
   const bool on = won.y > 0 && lost.y > 0;
   const double f[2] = {a.mean && on ? 1 / won.y : 1.0, a.mean && on ? 1 / lost.y : 1.0};
   const double S[2] = {won.x * f[0], lost.x * f[1]}, D = S[0] - S[1];
-  double loss = 0, slope = 0;
-  if (on) pair_term(a.kind, a.beta, a.smoothing, D, &loss, &slope);
-  slope *= a.scale;
+  const double slope = pair_slope(a.kind, a.beta, a.smoothing, D) * a.scale;
   const float grad = on ? (float)(s < a.pairs ? slope * f[0] : -slope * f[1]) : 0.f;
   const int64_t from = hold(a.offsets[s], a.tokens), to = hold(a.offsets[s + 1], a.tokens);
   for (int64_t i = from + ((int64_t)slice * G + threadIdx.x % G) * 4; i < to; i += (int64_t)g.slices * G * 4) {
@@ -157,19 +133,19 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
   if (s < a.pairs && slice == 0 && threadIdx.x % G == 0) {
     const double b = a.beta;
     if (a.margin) a.margin[k] = on ? (float)(b * D) : 0.f;
-    a.record[k] = on ? PairRecord{loss, D > 0 ? 1.0 : 0.0, b * D, b * S[0], b * S[1], 1.0} : PairRecord{0, 0, 0, 0, 0, 0};
+    a.record[k] = on ? PairRecord{pair_value(a.kind, a.beta, a.smoothing, D), D > 0 ? 1.0 : 0.0, b * D, b * S[0], b * S[1], 1.0} : PairRecord{0, 0, 0, 0, 0, 0};
   }
 }
 
 // stats: loss, share of pairs with D > 0, mean margin, mean chosen and rejected reward, active pairs, non-finite
 __global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRecord* rec, float scale, float* stats) {
-  __shared__ double lds[16];
+  __shared__ double lds[6 * 16];
   double v[6] = {0, 0, 0, 0, 0, 0};
   for (int64_t i = threadIdx.x; i < pairs; i += 1024) {
     const PairRecord r = rec[i];
     v[0] += r.loss; v[1] += r.right; v[2] += r.margin; v[3] += r.chosen; v[4] += r.rejected; v[5] += r.active;
   }
-  for (int k = 0; k < 6; ++k) v[k] = block_sum_d(v[k], lds);
+  block_sums<16>(v, lds);
   if (threadIdx.x) return;
   const double n = v[5] > 0 ? v[5] : 1;
   stats[0] = (float)(v[0] * scale);
@@ -182,15 +158,18 @@ __global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRe
 // A_t = r_t + gamma V' - V_t + gamma lambda A', where the primes are the next unmasked token of the sequence; behind the last
 // one V' is the sequence's last value (0 without one) and A' = 0.  R_t = A_t + V_t.  Masked tokens get 0.
 //
-// As maps of the pair (A, V) that comes from behind, a token is  A -> a A + b V + c,  V -> v or V (masked tokens: nothing
-// changes; the last token of a sequence first replaces the pair by (0, last value)), and maps of this form compose.  The tokens
-// are cut into tiles without regard to the sequences, so that the work is even whatever their lengths: k_gae_part composes the
-// maps of a tile, k_gae_tiles the tiles' maps from the end, k_token_gae applies what comes in to a tile's tokens.  With few tiles
-// the last one looks at the maps behind it by itself, and one tile needs nothing else.  A sum over a long sequence (gamma lambda
-// = 1) is held in 64 bits; 16 bytes a token move, so that the arithmetic does not show.
+// The tokens are cut into tiles without regard to the sequences, so that the work is even whatever their lengths.  A thread has
+// eight tokens in a row.  The V' of a thread's last token is the value in front of the nearest thread behind it that has an unmasked
+// token or the end of a sequence (a ballot finds it).  Then the tokens are maps A -> a A + c (masked ones: 1 and 0; the last token of a
+// sequence first replaces what comes in by 0), maps of this form compose, and a scan from the end gives every thread what comes in.
+// Of a tile as a whole, what comes from behind also enters through V': its map is A -> a A + b V + c, V -> v (or V).  k_gae_part
+// makes the tiles' maps, k_gae_tiles scans them, k_token_gae does the tokens; with few tiles the last one scans the maps behind its
+// own by itself, and one tile needs nothing else.  A sum over a long sequence (gamma lambda = 1) is held in 64 bits.
+//
+// Bound: 16 to 17 bytes a token, the inputs twice (from the last-level cache the second time) where there is more than one tile.
 constexpr int GAE_PER = 8, GAE_TILE = 256 * GAE_PER;   // tokens per thread and per tile
-constexpr int GAE_DIRECT = 512;                        // at most so many tiles are looked at directly
-struct GaeMap { double a, b, c, v; int32_t flags, pad; };     // flags: 1 = V -> v (else V stays), 2 = nothing from behind matters
+constexpr int GAE_DIRECT = 257;                        // at most so many tiles are scanned directly (256 maps, one per thread)
+struct GaeMap { double a, b, c; float v; int32_t set, stop, pad; };   // set: V -> v, else V stays; stop: nothing from behind matters
 struct GaeArgs {
   int64_t sequences, tokens;
   const float *reward, *value, *last_value;  // last_value: may be NULL
@@ -202,47 +181,65 @@ struct GaeArgs {
   GaeMap* map;                               // [tiles]
   double2* in;                               // [tiles] the pair (A, V) that enters a tile; NULL: direct
 };
-__device__ __forceinline__ GaeMap gae_nothing() { return GaeMap{1, 0, 0, 0, 0, 0}; }
-// first `behind`, then `m`
-__device__ __forceinline__ GaeMap then(const GaeMap& behind, const GaeMap& m) {
-  if (m.flags & 2) return m;
-  GaeMap o;
-  const bool set = behind.flags & 1;
-  o.a = m.a * behind.a;
-  o.b = m.a * behind.b + (set ? 0.0 : m.b);
-  o.c = m.a * behind.c + (set ? m.b * behind.v : 0.0) + m.c;
-  o.v = m.flags & 1 ? m.v : behind.v;
-  o.flags = m.flags | behind.flags;
-  o.pad = 0;
-  return o;
+// A -> a A + c; with a = 0 nothing of A matters, not even NaN: another sequence's is not to be seen
+struct Affine { double a, c; };
+__device__ __forceinline__ double apply(const Affine& m, double A) { return m.a == 0 ? m.c : m.a * A + m.c; }
+__device__ __forceinline__ Affine then(const Affine& behind, const Affine& m) { return Affine{m.a * behind.a, apply(m, behind.c)}; }
+template <int N> __device__ __forceinline__ double row_down(double old, double v) {   // of lane + N of the same 16, else `old`
+  const int lo = __builtin_amdgcn_update_dpp(__double2loint(old), __double2loint(v), DPP_ROW_SHL(N), 0xf, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(__double2hiint(old), __double2hiint(v), DPP_ROW_SHL(N), 0xf, 0xf, false);
+  return __hiloint2double(hi, lo);
 }
-__device__ __forceinline__ GaeMap shfl_down_map(const GaeMap& m, int o) {
-  return GaeMap{__shfl_down(m.a, o), __shfl_down(m.b, o), __shfl_down(m.c, o), __shfl_down(m.v, o), __shfl_down(m.flags, o), 0};
+template <int N> __device__ __forceinline__ Affine suffix_step(const Affine& m) {
+  return then(Affine{row_down<N>(1.0, m.a), row_down<N>(0.0, m.c)}, m);
 }
-// lane l: the maps of the lanes 63 .. l, composed
-__device__ __forceinline__ GaeMap wave_suffix(GaeMap m) {
-  const int lane = threadIdx.x & 63;
-  for (int o = 1; o < 64; o <<= 1) {
-    const GaeMap b = shfl_down_map(m, o);
-    if (lane + o < 64) m = then(b, m);
-  }
-  return m;
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
 }
-// The maps of all threads behind this one in the block, composed; *whole: those of the block.
+// What the threads behind this one (in a block of NW waves) do to A; *whole: what the block does.  One barrier.
 template <int NW>
-__device__ __forceinline__ GaeMap block_behind(const GaeMap& mine, GaeMap* lds, GaeMap* whole) {
+__device__ __forceinline__ Affine block_behind(const Affine& mine, Affine* lds, Affine* whole) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const GaeMap suf = wave_suffix(mine);
-  if (lane == 0) lds[wave] = suf;
+  Affine m = mine;                          // on the way: the lanes of the same 16 from this one on
+  m = suffix_step<1>(m); m = suffix_step<2>(m); m = suffix_step<4>(m); m = suffix_step<8>(m);
+  const Affine r3 = {lane_value(m.a, 48), lane_value(m.c, 48)};
+  const Affine r2 = then(r3, Affine{lane_value(m.a, 32), lane_value(m.c, 32)});
+  const Affine r1 = then(r2, Affine{lane_value(m.a, 16), lane_value(m.c, 16)});
+  const Affine one = {1.0, 0.0};
+  const Affine far = lane >= 48 ? one : lane >= 32 ? r3 : lane >= 16 ? r2 : r1;
+  m = then(far, m);                         // the lanes of the wave from this one on
+  if (lane == 0) lds[wave] = m;
   __syncthreads();
-  GaeMap behind = gae_nothing(), all = gae_nothing();
+  Affine behind = one, all = one;
+#pragma unroll 4
   for (int w = NW - 1; w >= 0; --w) {
     if (w == wave) behind = all;
     all = then(all, lds[w]);
   }
   if (whole) *whole = all;
-  const GaeMap next = shfl_down_map(suf, 1);
+  const Affine next = {__shfl_down(m.a, 1), __shfl_down(m.c, 1)};
   return lane < 63 ? then(behind, next) : behind;
+}
+// The value that enters a thread from behind: that in front of the nearest thread behind it which has one (set), or `in`.  *front, *any:
+// what leaves the block, and whether it is the block's own.  One barrier.
+template <int NW>
+__device__ __forceinline__ double block_value(bool set, double v, double in, double* lds_v, int* lds_set, double* front, bool* any) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t who = __ballot(set);
+  if (set && lane == __ffsll((unsigned long long)who) - 1) lds_v[wave] = v;
+  if (lane == 0) lds_set[wave] = who != 0;
+  __syncthreads();
+  const uint64_t above = lane == 63 ? 0 : who >> (lane + 1);
+  const double near = __shfl(v, above ? lane + __ffsll((unsigned long long)above) : 0);
+  double x = in, out = in;
+  bool found = false;
+#pragma unroll 4
+  for (int w = NW - 1; w >= 0; --w) {
+    if (w == wave) x = out;
+    if (lds_set[w]) { out = lds_v[w]; found = true; }
+  }
+  if (front) { *front = out; *any = found; }
+  return above ? near : x;
 }
 
 // The first k of [0, n) with offsets[k] > at (n: none), by the lanes of a wave together: 64 places are looked at per step.
@@ -296,72 +293,105 @@ __device__ __forceinline__ void gae_load(const GaeArgs& a, int64_t tile, int32_t
   t.on &= t.in;
 }
 __device__ __forceinline__ double gae_last(const GaeArgs& a, int32_t end) { return a.last_value ? (double)a.last_value[end - 1] : 0.0; }
-// the map of a thread's tokens
-__device__ __forceinline__ GaeMap gae_map(const GaeArgs& a, const GaeTile& t) {
-  GaeMap m = gae_nothing();
+// whether a thread's tokens hide what comes from behind, and the value in front of them then
+__device__ __forceinline__ bool gae_front(const GaeArgs& a, const GaeTile& t, double* v) {
+  bool set = false;
+#pragma unroll
+  for (int k = GAE_PER - 1; k >= 0; --k) {
+    if (t.end[k]) { set = true; *v = gae_last(a, t.end[k]); }
+    if (t.on >> k & 1) { set = true; *v = t.v[k]; }
+  }
+  return set;
+}
+// what a thread's tokens do to A, V being what enters them
+__device__ __forceinline__ Affine gae_map(const GaeArgs& a, const GaeTile& t, double V) {
+  Affine m = {1.0, 0.0};
   const double gl = a.gamma * a.lambda;
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) {
-    if (t.end[k]) m = GaeMap{0, 0, 0, gae_last(a, t.end[k]), 3, 0};
+    if (t.end[k]) { m = Affine{0.0, 0.0}; V = gae_last(a, t.end[k]); }
     if (t.on >> k & 1) {
-      const bool set = m.flags & 1;
       const double v = t.v[k];
-      m.c = gl * m.c + (set ? a.gamma * m.v : 0.0) + ((double)t.r[k] - v);
-      m.b = gl * m.b + (set ? 0.0 : a.gamma);
-      m.a *= gl;
-      m.v = v;
-      m.flags |= 1;
+      m = Affine{gl * m.a, gl * m.c + (a.gamma * V + ((double)t.r[k] - v))};
+      V = v;
     }
   }
   return m;
 }
-__device__ __forceinline__ double2 gae_apply(const GaeMap& m, double2 in) {
-  if (m.flags & 2) return make_double2(m.c, m.v);
-  return make_double2(m.a * in.x + m.b * in.y + m.c, m.flags & 1 ? m.v : in.y);
-}
 
 __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
   __shared__ int32_t ends[GAE_TILE];
-  __shared__ GaeMap lds[4];
+  __shared__ Affine lds[4];
+  __shared__ double lds_v[4];
+  __shared__ int lds_set[4];
+  __shared__ int count, stops;
+  if (threadIdx.x == 0) count = stops = 0;
   GaeTile t;
-  gae_load(a, blockIdx.x, ends, t);
-  GaeMap whole;
-  block_behind<4>(gae_map(a, t), lds, &whole);
-  if (threadIdx.x == 0) a.map[blockIdx.x] = whole;
+  gae_load(a, blockIdx.x, ends, t);   // with barriers
+  double v = 0, front;
+  bool any, stop = false;
+  const bool set = gae_front(a, t, &v);
+#pragma unroll
+  for (int k = 0; k < GAE_PER; ++k) stop |= t.end[k] != 0;
+  if (t.on) atomicAdd(&count, __popc(t.on));
+  if (stop) stops = 1;
+  const double V = block_value<4>(set, v, 0.0, lds_v, lds_set, &front, &any);
+  Affine whole;
+  block_behind<4>(gae_map(a, t, V), lds, &whole);
+  if (threadIdx.x == 0) {
+    // without the end of a sequence in the tile, V comes into the last of its n unmasked tokens, and n - 1 more times gamma lambda
+    const double gl = a.gamma * a.lambda;
+    const double b = stops || count == 0 ? 0.0 : count == 1 ? a.gamma : gl > 0 ? whole.a / gl * a.gamma : 0.0;
+    a.map[blockIdx.x] = GaeMap{stops ? 0.0 : whole.a, b, whole.c, (float)front, any, stops, 0};
+  }
 }
 
+// The pair that enters the tile in front of `n` maps, by a block of NW waves, one map a thread (the farthest in the last thread), `far`
+// being the pair that enters the last of them.  The pair that enters this thread's tile goes to *mine.
+template <int NW>
+__device__ __forceinline__ double2 gae_tiles(const GaeMap& m, double2 far, double2* mine, Affine* lds, double* lds_v, int* lds_set) {
+  double front;
+  bool any;
+  const double V = block_value<NW>(m.set, m.v, far.y, lds_v, lds_set, &front, &any);
+  Affine whole;
+  const Affine behind = block_behind<NW>(Affine{m.a, m.b == 0 ? m.c : m.c + m.b * V}, lds, &whole);
+  if (mine) *mine = make_double2(apply(behind, far.x), V);
+  return make_double2(apply(whole, far.x), front);
+}
+__device__ __forceinline__ GaeMap gae_nothing() { return GaeMap{1, 0, 0, 0, 0, 0, 0}; }
+
 __global__ __launch_bounds__(1024) void k_gae_tiles(GaeArgs a) {
-  __shared__ GaeMap lds[16];
-  double2 carry = make_double2(0, 0);
+  __shared__ Affine lds[16];
+  __shared__ double lds_v[16];
+  __shared__ int lds_set[16];
+  double2 far = make_double2(0, 0);
   for (int64_t from = (a.tiles - 1) / 1024 * 1024; from >= 0; from -= 1024) {
     const int64_t k = from + threadIdx.x;
-    GaeMap whole;
-    const GaeMap behind = block_behind<16>(k < a.tiles ? a.map[k] : gae_nothing(), lds, &whole);
-    if (k < a.tiles) a.in[k] = gae_apply(behind, carry);
-    carry = gae_apply(whole, carry);
-    __syncthreads();   // lds is written again
+    double2 mine;
+    far = gae_tiles<16>(k < a.tiles ? a.map[k] : gae_nothing(), far, &mine, lds, lds_v, lds_set);
+    if (k < a.tiles) a.in[k] = mine;
+    __syncthreads();   // the LDS is written again
   }
 }
 
 __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
   __shared__ int32_t ends[GAE_TILE];
-  __shared__ GaeMap lds[4];
+  __shared__ Affine lds[2][4];
+  __shared__ double lds_v[2][4];
+  __shared__ int lds_set[2][4];
   const int64_t tile = blockIdx.x;
   double2 in = make_double2(0, 0);
   if (a.in) in = a.in[tile];
-  else {
-    GaeMap m = gae_nothing();
-    for (int64_t k = tile + 1; k < a.tiles && !(m.flags & 2); k += 64) {
-      const int64_t j = k + (threadIdx.x & 63);
-      const GaeMap far = wave_suffix(j < a.tiles ? a.map[j] : gae_nothing());
-      m = then(GaeMap{__shfl(far.a, 0), __shfl(far.b, 0), __shfl(far.c, 0), __shfl(far.v, 0), __shfl(far.flags, 0), 0}, m);
-    }
-    in = gae_apply(m, in);
+  else if (tile + 1 < a.tiles) {
+    const int64_t k = tile + 1 + threadIdx.x;
+    in = gae_tiles<4>(k < a.tiles ? a.map[k] : gae_nothing(), in, nullptr, lds[1], lds_v[1], lds_set[1]);
   }
   GaeTile t;
   gae_load(a, tile, ends, t);
-  in = gae_apply(block_behind<4>(gae_map(a, t), lds, nullptr), in);
-  double A = in.x, V = in.y;
+  double v = 0;
+  const bool set = gae_front(a, t, &v);
+  double V = block_value<4>(set, v, in.y, lds_v[0], lds_set[0], nullptr, nullptr);
+  double A = apply(block_behind<4>(gae_map(a, t, V), lds[0], nullptr), in.x);
   const double gl = a.gamma * a.lambda;
   float adv[GAE_PER], ret[GAE_PER];
 #pragma unroll
@@ -369,7 +399,7 @@ __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
     if (t.end[k]) { A = 0; V = gae_last(a, t.end[k]); }
     const bool on = t.on >> k & 1;
     const double v = t.v[k];
-    if (on) { A = gl * A + a.gamma * V + ((double)t.r[k] - v); V = v; }
+    if (on) { A = gl * A + (a.gamma * V + ((double)t.r[k] - v)); V = v; }
     adv[k] = on ? (float)A : 0.f;
     ret[k] = on ? (float)(A + v) : 0.f;
   }

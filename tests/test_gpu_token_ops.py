@@ -33,6 +33,12 @@ def matrix(rows, cols, dtype, seed, pad=0, shift=0, scale=3.0):
     return m, store
 
 
+def copy_in_place(x, store):
+    """A copy of the matrix x, which lies in `store`, at the same alignment and row stride (a row's sums are added up in an order that
+    goes by its alignment)."""
+    return store.clone().as_strided(x.shape, x.stride(), x.storage_offset())
+
+
 # ------------------------------------------------------------------------------------------------------------ rows of logits
 
 def row_definition(x, target, temperature):
@@ -128,7 +134,7 @@ def gradient_tolerance(grad, size, d, tol, V, dtype):
 def test_token_logp_backward(rows, vocab, dtype):
     dt = TYPES[dtype]
     for k, (temperature, pad, shift, kind) in enumerate(((1.0, 0, 0, "plain"), (0.7, 3, 1, "banned"), (1.3, 1, 5, "lowest"))):
-        x, _, target = logits_case(rows, vocab, dt, 100 * k + rows, pad, shift, kind)
+        x, store, target = logits_case(rows, vocab, dt, 100 * k + rows, pad, shift, kind)
         active, at, d, p, _, ent = row_definition(x, target, temperature)
         tol, tol_ent = row_tolerance(d, p, at, vocab)
         g, h = (torch.randn(rows, generator=rnd(7 + q), device="cuda") for q in range(2))
@@ -147,7 +153,7 @@ def test_token_logp_backward(rows, vocab, dtype):
             inside = torch.zeros_like(now, dtype=torch.bool)
             inside[3:3 + rows * (vocab + 2 * pad)].view(rows, -1)[:, :vocab] = True
             assert torch.equal(now[~inside].view(torch.uint8), frame[~inside].view(torch.uint8))
-        there = x.clone()
+        there = copy_in_place(x, store)
         here = L.token_logp_backward(there, target, stat, g, temperature=temperature, out=there)
         assert here.data_ptr() == there.data_ptr()
         assert torch.equal(there, L.token_logp_backward(x, target, stat, g, temperature=temperature)), "in the logits' own memory"
@@ -181,7 +187,7 @@ def test_token_loss(rows, vocab, dtype):
     dt = TYPES[dtype]
     for k, (temperature, pad, shift, kind, kl_coef, ent_coef, weighted) in enumerate((
             (1.0, 0, 0, "plain", 0.0, 0.0, False), (0.7, 3, 1, "banned", 0.1, 0.02, True), (1.3, 1, 5, "lowest", 0.05, 0.0, True), (1.0, 0, 0, "banned", 0.0, 0.3, False))):
-        x, _, target = logits_case(rows, vocab, dt, 100 * k + rows, pad, shift, kind)
+        x, store, target = logits_case(rows, vocab, dt, 100 * k + rows, pad, shift, kind)
         base = row_definition(x, target, temperature)[4]
         noise = lambda q, a: (a * torch.randn(rows, generator=rnd(q), device="cuda"))  # noqa: E731
         old, ref, adv = (base + noise(11, 0.2)).float(), (base + noise(12, 0.4)).float(), noise(13, 1.0)
@@ -214,7 +220,7 @@ def test_token_loss(rows, vocab, dtype):
             size_q = term + abs(b) if q < 4 else 1 + abs(b)
             assert abs(a - b) <= slack * (size_q + (w.abs() * (ref_rho + ent)).sum().item()) + 4 * U32 * abs(b), (q, a, b)
         assert got_stats[6].item() == stats[6]
-        there = x.clone()
+        there = copy_in_place(x, store)
         assert torch.equal(L.token_loss(there, target, old, adv, logp_ref=use_ref, weight=weight, out=there, **hp)[0], got), "in the logits' own memory, and twice the same"
 
 
@@ -268,7 +274,8 @@ def test_rows_far_apart():
     x = store.as_strided((3, V), (ld, 1))
     x.copy_(torch.randn(3, V, device="cuda", generator=rnd(5)))
     t = torch.tensor([1, 2, 1000], dtype=torch.int32, device="cuda")
-    near = x.contiguous()
+    near = torch.empty(3, 1008, dtype=torch.bfloat16, device="cuda")[:, :V]   # rows at 16-byte boundaries, as x has them
+    near.copy_(x)
     z = torch.zeros(3, device="cuda")
     for a, b in zip(L.token_logp(x, t, want_entropy=True), L.token_logp(near, t, want_entropy=True)):
         assert torch.equal(a, b)
