@@ -19,6 +19,7 @@ __device__ __forceinline__ void forget(u32x4_t& v) { asm volatile("" : "+v"(v));
 template <class T> struct Piece { static constexpr int N = 16 / sizeof(T); };
 template <class T> __device__ __forceinline__ u32x4_t load_piece(const T* p) { return *reinterpret_cast<const u32x4_any_t*>(p); }
 template <class T> __device__ __forceinline__ void store_piece(T* p, u32x4_t v) { *reinterpret_cast<u32x4_any_t*>(p) = v; }
+template <class T> __device__ __forceinline__ void store_piece_past_caches(T* p, u32x4_t v) { __builtin_nontemporal_store(v, reinterpret_cast<u32x4_any_t*>(p)); }
 __device__ __forceinline__ void unpack(u32x4_t v, float (&f)[4], float) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);

@@ -71,15 +71,17 @@ int check_sizes(int32_t dtype, int64_t rows, int64_t vocab) {
   return PPO_OK;
 }
 
-// Rows in slices (k_token_part and what follows it): where whole rows would leave most of the chip idle.
-constexpr int MAX_SLICES = 64;
-int slices_of(int64_t rows, int64_t vocab) {
-  if (rows >= 256 || vocab < 8192) return 1;
+// Rows in slices (k_token_part and what follows it): long rows that would leave part of the chip idle.  One more launch, 2 us, buys
+// the other CUs' arithmetic: 16 rows of 128000 take 8 us in slices and 13 whole (loss: 14 and 18), 200 rows 14 and 17 (loss: 31 and 25),
+// 16 rows of 32000 9 and 7 (14 and 11).
+constexpr int MAX_SLICES = 64, SLICED_ROWS = 255, SLICED_LOSS_ROWS = 96;
+int slices_of(int64_t rows, int64_t vocab, int64_t most_rows) {
+  if (rows > most_rows || vocab <= 40960) return 1;
   return (int)std::min<int64_t>(std::min<int64_t>(cdiv(1024, rows), cdiv(vocab, 4096)), MAX_SLICES);
 }
 // slices of a multiple of 64 elements, all but the last of one length, none empty
-void set_slices(RowArgs& a) {
-  const int s = slices_of(a.rows, a.vocab);
+void set_slices(RowArgs& a, int64_t most_rows) {
+  const int s = slices_of(a.rows, a.vocab, most_rows);
   a.slice_len = (int32_t)(cdiv(cdiv(a.vocab, s), 64) * 64);
   a.slices = (int32_t)cdiv(a.vocab, a.slice_len);
 }
@@ -87,7 +89,7 @@ void set_slices(RowArgs& a) {
 // Workspace of a call on rows: parts of the slices (16 bytes each), records of the loss, then sums of the blocks that add those up.
 int stats_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, STATS_ROWS), 1024)); }
 int64_t stats_offset(int64_t rows, int64_t vocab) {
-  const int s = slices_of(std::max<int64_t>(rows, 1), vocab);
+  const int s = slices_of(std::max<int64_t>(rows, 1), vocab, SLICED_ROWS);
   return ((s > 1 ? rows * s * 16 : 0) + rows * (int64_t)sizeof(LossRecord) + 15) / 16 * 16;
 }
 
@@ -137,6 +139,7 @@ void launch_loss(const RowArgs& a, hipStream_t st) {
   LOSS(256, 16)
   LOSS(512, 16)
   LOSS(1024, 16)
+  LOSS(1024, 24)
 #undef LOSS
   hipLaunchKernelGGL((k_token_loss_long<T, ENT>), dim3((uint32_t)a.rows), dim3(1024), 0, st, a);
 }
@@ -196,7 +199,7 @@ int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   a.rows = rows; a.ld = ld; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
   a.logp = d_logp; a.entropy = d_entropy; a.stat = d_stat;
   a.part = (float*)d_ws;
-  set_slices(a);
+  set_slices(a, SLICED_ROWS);
   hipStream_t st = (hipStream_t)hip_stream;
   with_type(dtype, [&](auto t) {
     with_flag(d_entropy != nullptr, [&](auto ent) {
@@ -237,10 +240,13 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
       using T = decltype(t);
       constexpr bool ENT = decltype(ent)::value;
       const int64_t pieces = cdiv(vocab, Piece<T>::N);
-      if (pieces <= 16 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 16, ENT>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
-      else if (pieces <= 64 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 64, ENT>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
-      else hipLaunchKernelGGL((k_token_logp_backward<T, 256, ENT>), dim3((uint32_t)cdiv(pieces, 256 * BACK_PIECES), (uint32_t)std::min<int64_t>(rows, 65535), (uint32_t)cdiv(rows, 65535)),
-                              dim3(256), 0, st, a);
+      with_flag(rows * vocab * (int64_t)sizeof(T) > PAST_BYTES, [&](auto past) {
+        constexpr bool PAST = decltype(past)::value;
+        if (pieces <= 16 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 16, ENT, PAST>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
+        else if (pieces <= 64 * BACK_PIECES) hipLaunchKernelGGL((k_token_logp_backward<T, 64, ENT, PAST>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((k_token_logp_backward<T, 256, ENT, PAST>), dim3((uint32_t)cdiv(pieces, 256 * BACK_PIECES), (uint32_t)std::min<int64_t>(rows, 65535), (uint32_t)cdiv(rows, 65535)),
+                                dim3(256), 0, st, a);
+      });
     });
   });
   LAUNCHCHK("k_token_logp_backward");
@@ -273,9 +279,10 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / hp->temperature;
   a.logp = d_logp; a.dlogits = d_dlogits; a.logp_old = d_logp_old; a.logp_ref = d_logp_ref; a.adv = d_adv; a.weight = d_weight;
   a.clip_lo = hp->clip_lo; a.clip_hi = hp->clip_hi; a.kl_coef = hp->kl_coef; a.ent_coef = hp->ent_coef; a.scale = hp->scale;
+ 
   hipStream_t st = (hipStream_t)hip_stream;
   if (rows > 0) {
-    set_slices(a);
+    set_slices(a, SLICED_LOSS_ROWS);
     a.part = (float*)d_ws;
     a.record = (float*)d_ws + (a.slices > 1 ? rows * a.slices * 4 : 0);
     with_type(dtype, [&](auto t) {

@@ -235,16 +235,22 @@ __device__ __forceinline__ void zero_row(T* y, int n, int tid, int G) {
 
 // Gradient of the log-probability and the entropy from the row's statistics: every piece by itself.  A group of G threads does a
 // slice of G BACK_PIECES pieces of a row: blockIdx.x the slice (G < 256: the row is one slice), blockIdx.y and z the row.
+// PAST: stored past the caches, for gradients that are larger than the last-level cache: they would only push out the logits, which the
+// forward pass has just read (gradient of 524 MB, 32 bits: forward and backward 311 -> 267 us).  Smaller ones are read from that cache by
+// whatever comes next (65 MB: 46 us with that reader, 50 past the caches).
+constexpr int64_t PAST_BYTES = 256000000;
 constexpr int BACK_PIECES = 4;   // pieces per thread
-template <class T, int G, bool ENT>
+template <class T, int G, bool ENT, bool PAST>
 __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
   constexpr int N = Piece<T>::N;
-  const int64_t row = G < 256 ? (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G : blockIdx.y + (int64_t)blockIdx.z * 65535;
-  if (row >= a.rows) return;
+  const int64_t back = G < 256 ? (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G : blockIdx.y + (int64_t)blockIdx.z * 65535;
+  if (back >= a.rows) return;
+  const int64_t row = a.rows - 1 - back;   // the rows that the forward pass read last are still in the last-level cache
   const int t = a.target[row], from = (G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N)) + threadIdx.x % G * N;
   const int tid = threadIdx.x % G;
   const T* x = (const T*)a.logits + row * a.ld;
   T* y = (T*)a.dlogits + row * a.ldd;
+  const auto store = [](T* p, u32x4_t v) { if constexpr (PAST) store_piece_past_caches(p, v); else store_piece(p, v); };
   Cut q = cut_row(x, a.vocab, tid);
   if (G >= 256 && blockIdx.x) q.one = -1;   // the first slice's threads take head and tail
   const float mx = a.stat[2 * row], ls = a.stat[2 * row + 1];
@@ -252,7 +258,7 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
     const u32x4_t z = {0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < BACK_PIECES; ++u)
-      if (from + u * G * N < q.full) store_piece(y + q.head + from + u * G * N, z);
+      if (from + u * G * N < q.full) store(y + q.head + from + u * G * N, z);
     if (q.one >= 0) y[q.one] = from_f<T>(0.f);
     return;
   }
@@ -268,7 +274,7 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
     if (from + u * G * N < q.full) v[u] = load_piece(x + q.head + from + u * G * N);
 #pragma unroll
   for (int u = 0; u < BACK_PIECES; ++u)
-    if (from + u * G * N < q.full) store_piece(y + q.head + from + u * G * N, grad_piece<T, ENT>(v[u], k));
+    if (from + u * G * N < q.full) store(y + q.head + from + u * G * N, grad_piece<T, ENT>(v[u], k));
   if (q.one >= 0) y[q.one] = from_f<T>(grad_one<ENT>(xl, k));
   if (owner) y[t] = from_f<T>(grad_one<ENT>(xt, k) + k.add);
 }
@@ -319,7 +325,7 @@ __device__ __forceinline__ void loss_idle(const RowArgs& a, int64_t row) {
 // Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers between the pass that
 // adds up and the one that writes, so that memory sees it once in and once out.
 template <class T, int G, int K, bool ENT>
-__global__ __launch_bounds__(G < 256 ? 256 : G, K == 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
+__global__ __launch_bounds__(G < 256 ? 256 : G, K >= 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
   constexpr int NT = G < 256 ? 256 : G, N = Piece<T>::N;
   __shared__ float lds[3 * (NT / 64)];
   const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);

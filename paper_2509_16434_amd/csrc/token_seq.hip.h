@@ -82,14 +82,20 @@ __global__ __launch_bounds__(256) void k_pair_sums(PairArgs a, PairGrid g) {
   const int64_t from = hold(a.offsets[s], a.tokens), to = hold(a.offsets[s + 1], a.tokens);
   double v = 0;
   int c = 0;
-  for (int64_t i = from + ((int64_t)slice * G + threadIdx.x % G) * 4; i < to; i += (int64_t)g.slices * G * 4) {
+  // groups of four tokens between boundaries of four, so that all but the arrays' last one are read whole
+  const int64_t step = (int64_t)g.slices * G * 4;
+  for (int64_t i = (from & ~(int64_t)3) + ((int64_t)slice * G + threadIdx.x % G) * 4; i < to; i += step) {
     float x[4], r[4] = {0.f, 0.f, 0.f, 0.f};
     bool on[4];
-    load4(a.logp, i, to, x);
-    if (a.ref) load4(a.ref, i, to, r);
-    mask4(a.mask, i, to, on);
+    load4(a.logp, i, a.tokens, x);
+    if (a.ref) load4(a.ref, i, a.tokens, r);
+    mask4(a.mask, i, a.tokens, on);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { v += on[k] ? (double)x[k] - (double)r[k] : 0.0; c += on[k]; }
+    for (int k = 0; k < 4; ++k) {
+      const bool count = on[k] && i + k >= from && i + k < to;
+      v += count ? (double)x[k] - (double)r[k] : 0.0;
+      c += count;
+    }
   }
   double sums[2] = {v, (double)c};
   block_sums<G / 64>(sums, lds);
@@ -122,13 +128,19 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
   const double slope = pair_slope(a.kind, a.beta, a.smoothing, D) * a.scale;
   const float grad = on ? (float)(s < a.pairs ? slope * f[0] : -slope * f[1]) : 0.f;
   const int64_t from = hold(a.offsets[s], a.tokens), to = hold(a.offsets[s + 1], a.tokens);
-  for (int64_t i = from + ((int64_t)slice * G + threadIdx.x % G) * 4; i < to; i += (int64_t)g.slices * G * 4) {
+  const int64_t step = (int64_t)g.slices * G * 4;
+  for (int64_t i = (from & ~(int64_t)3) + ((int64_t)slice * G + threadIdx.x % G) * 4; i < to; i += step) {
     bool m[4];
     float d[4];
-    mask4(a.mask, i, to, m);
+    mask4(a.mask, i, a.tokens, m);
 #pragma unroll
     for (int q = 0; q < 4; ++q) d[q] = m[q] ? grad : 0.f;
-    store4(a.dlogp, i, to, d);
+    if (i >= from && i + 4 <= to) store4(a.dlogp, i, to, d);
+    else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        if (i + q >= from && i + q < to) a.dlogp[i + q] = d[q];
+    }
   }
   if (s < a.pairs && slice == 0 && threadIdx.x % G == 0) {
     const double b = a.beta;
@@ -168,8 +180,9 @@ __global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRe
 //
 // Bound: 16 to 17 bytes a token, the inputs twice (from the last-level cache the second time) where there is more than one tile.
 constexpr int GAE_PER = 8, GAE_TILE = 256 * GAE_PER;   // tokens per thread and per tile
-constexpr int GAE_DIRECT = 257;                        // at most so many tiles are scanned directly (256 maps, one per thread)
-struct GaeMap { double a, b, c; float v; int32_t set, stop, pad; };   // set: V -> v, else V stays; stop: nothing from behind matters
+constexpr int GAE_DIRECT = 4096;                       // at most so many tiles are scanned directly
+struct GaeMap { double a, b, c; float v; int32_t set, stop, offset; };   // set: V -> v, else V stays; stop: nothing from behind
+                                                                       // matters; offset: first_above at the tile's start
 struct GaeArgs {
   int64_t sequences, tokens;
   const float *reward, *value, *last_value;  // last_value: may be NULL
@@ -262,7 +275,8 @@ struct GaeTile {
   uint32_t on, in;          // bit k: the token counts; it lies in a sequence
   int32_t end[GAE_PER];     // 1 + its sequence, if it is that one's last token; else 0
 };
-__device__ __forceinline__ void gae_load(const GaeArgs& a, int64_t tile, int32_t* ends, GaeTile& t) {
+// offset: first_above at the tile's start, or -1: it is looked for, and returned
+__device__ __forceinline__ int64_t gae_load(const GaeArgs& a, int64_t tile, int64_t offset, int32_t* ends, GaeTile& t) {
   const int64_t start = tile * GAE_TILE, stop = start + GAE_TILE < a.tokens ? start + GAE_TILE : a.tokens;
   const int64_t i = start + threadIdx.x * GAE_PER;
   t.on = t.in = 0;
@@ -279,7 +293,8 @@ __device__ __forceinline__ void gae_load(const GaeArgs& a, int64_t tile, int32_t
   for (int k = threadIdx.x; k < GAE_TILE; k += 256) ends[k] = 0;
   __syncthreads();
   const int64_t first = a.sequences ? hold(a.offsets[0], a.tokens) : a.tokens, last = hold(a.offsets[a.sequences], a.tokens);
-  for (int64_t j = first_above(a.offsets, a.sequences + 1, a.tokens, start) + threadIdx.x; j <= a.sequences; j += 256) {
+  if (offset < 0) offset = first_above(a.offsets, a.sequences + 1, a.tokens, start);
+  for (int64_t j = offset + threadIdx.x; j <= a.sequences; j += 256) {
     const int64_t o = hold(a.offsets[j], a.tokens);
     if (o > start + GAE_TILE) break;
     if (j > 0 && o > start && o > hold(a.offsets[j - 1], a.tokens)) ends[o - 1 - start] = (int32_t)j;
@@ -291,6 +306,7 @@ __device__ __forceinline__ void gae_load(const GaeArgs& a, int64_t tile, int32_t
     t.in |= (uint32_t)(i + k >= first && i + k < last) << k;
   }
   t.on &= t.in;
+  return offset;
 }
 __device__ __forceinline__ double gae_last(const GaeArgs& a, int32_t end) { return a.last_value ? (double)a.last_value[end - 1] : 0.0; }
 // whether a thread's tokens hide what comes from behind, and the value in front of them then
@@ -327,7 +343,7 @@ __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
   __shared__ int count, stops;
   if (threadIdx.x == 0) count = stops = 0;
   GaeTile t;
-  gae_load(a, blockIdx.x, ends, t);   // with barriers
+  const int64_t offset = gae_load(a, blockIdx.x, -1, ends, t);   // with barriers
   double v = 0, front;
   bool any, stop = false;
   const bool set = gae_front(a, t, &v);
@@ -342,7 +358,7 @@ __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
     // without the end of a sequence in the tile, V comes into the last of its n unmasked tokens, and n - 1 more times gamma lambda
     const double gl = a.gamma * a.lambda;
     const double b = stops || count == 0 ? 0.0 : count == 1 ? a.gamma : gl > 0 ? whole.a / gl * a.gamma : 0.0;
-    a.map[blockIdx.x] = GaeMap{stops ? 0.0 : whole.a, b, whole.c, (float)front, any, stops, 0};
+    a.map[blockIdx.x] = GaeMap{stops ? 0.0 : whole.a, b, whole.c, (float)front, any, stops, (int32_t)offset};
   }
 }
 
@@ -383,11 +399,23 @@ __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
   double2 in = make_double2(0, 0);
   if (a.in) in = a.in[tile];
   else if (tile + 1 < a.tiles) {
-    const int64_t k = tile + 1 + threadIdx.x;
-    in = gae_tiles<4>(k < a.tiles ? a.map[k] : gae_nothing(), in, nullptr, lds[1], lds_v[1], lds_set[1]);
+    // 256 maps at a time: first up to those among which nothing from behind matters any more (mostly the first ones), then back
+    int64_t k = tile + 1 + threadIdx.x;
+    GaeMap m = k < a.tiles ? a.map[k] : gae_nothing();
+    while (k - threadIdx.x + 256 < a.tiles && !__syncthreads_or(m.stop)) {
+      k += 256;
+      m = k < a.tiles ? a.map[k] : gae_nothing();
+    }
+    for (;;) {
+      in = gae_tiles<4>(m, in, nullptr, lds[1], lds_v[1], lds_set[1]);
+      if (k <= tile + 256) break;
+      k -= 256;
+      m = a.map[k];
+      __syncthreads();   // the LDS is written again
+    }
   }
   GaeTile t;
-  gae_load(a, tile, ends, t);
+  gae_load(a, tile, a.tiles > 1 ? a.map[tile].offset : -1, ends, t);
   double v = 0;
   const bool set = gae_front(a, t, &v);
   double V = block_value<4>(set, v, in.y, lds_v[0], lds_set[0], nullptr, nullptr);
