@@ -272,52 +272,65 @@ __device__ __forceinline__ int64_t first_above(const int64_t* offsets, int64_t n
 // A tile's tokens in registers: eight in a row per thread.
 struct GaeTile {
   float r[GAE_PER], v[GAE_PER];
-  uint32_t on, in;          // bit k: the token counts; it lies in a sequence
-  int32_t end[GAE_PER];     // 1 + its sequence, if it is that one's last token; else 0
+  float last[GAE_PER];      // the last value of the sequence that ends with the token
+  uint32_t on, end;         // bit k: the token counts; it is a sequence's last one
 };
-// offset: first_above at the tile's start, or -1: it is looked for, and returned
-__device__ __forceinline__ int64_t gae_load(const GaeArgs& a, int64_t tile, int64_t offset, int32_t* ends, GaeTile& t) {
-  const int64_t start = tile * GAE_TILE, stop = start + GAE_TILE < a.tokens ? start + GAE_TILE : a.tokens;
-  const int64_t i = start + threadIdx.x * GAE_PER;
-  t.on = t.in = 0;
+// What ends in a tile: a bit per token, and the last values where one is set.
+struct GaeEnds { uint32_t bits[GAE_TILE / 32]; float last[GAE_TILE]; };
+// offset: first_above at the tile's start, or -1: it is looked for, and returned.  Two barriers.
+__device__ __forceinline__ int64_t gae_load(const GaeArgs& a, int64_t tile, int64_t offset, GaeEnds& ends, GaeTile& t) {
+  const int64_t start = tile * GAE_TILE, i = start + threadIdx.x * GAE_PER;
+  t.on = 0;
+  if (start + GAE_TILE <= a.tokens) {   // all but the last tile
 #pragma unroll
-  for (int h = 0; h < GAE_PER; h += 4) {
-    bool on[4];
-    float r[4], v[4];
-    mask4(a.mask, i + h, stop, on);
-    load4(a.reward, i + h, stop, r);
-    load4(a.value, i + h, stop, v);
+    for (int h = 0; h < GAE_PER; h += 4) {
+      const f32x4_any_t r = *reinterpret_cast<const f32x4_any_t*>(a.reward + i + h), v = *reinterpret_cast<const f32x4_any_t*>(a.value + i + h);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) { t.r[h + k] = r[k]; t.v[h + k] = v[k]; t.on |= (uint32_t)on[k] << (h + k); }
+      for (int k = 0; k < 4; ++k) { t.r[h + k] = r[k]; t.v[h + k] = v[k]; }
+    }
+    if (a.mask) {
+      const u8x4_any_t m0 = *reinterpret_cast<const u8x4_any_t*>(a.mask + i), m1 = *reinterpret_cast<const u8x4_any_t*>(a.mask + i + 4);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t.on |= (uint32_t)(m0[k] != 0) << k | (uint32_t)(m1[k] != 0) << (k + 4);
+    } else t.on = 0xff;
+  } else {
+#pragma unroll
+    for (int k = 0; k < GAE_PER; ++k) {
+      const bool in = i + k < a.tokens;
+      t.r[k] = in ? a.reward[i + k] : 0.f;
+      t.v[k] = in ? a.value[i + k] : 0.f;
+      t.on |= (uint32_t)(in && (!a.mask || a.mask[i + k])) << k;
+    }
   }
-  for (int k = threadIdx.x; k < GAE_TILE; k += 256) ends[k] = 0;
+  if (threadIdx.x < GAE_TILE / 32) ends.bits[threadIdx.x] = 0;
   __syncthreads();
   const int64_t first = a.sequences ? hold(a.offsets[0], a.tokens) : a.tokens, last = hold(a.offsets[a.sequences], a.tokens);
   if (offset < 0) offset = first_above(a.offsets, a.sequences + 1, a.tokens, start);
   for (int64_t j = offset + threadIdx.x; j <= a.sequences; j += 256) {
-    const int64_t o = hold(a.offsets[j], a.tokens);
+    const int64_t o = hold(a.offsets[j], a.tokens), before = j > 0 ? hold(a.offsets[j - 1], a.tokens) : o;
     if (o > start + GAE_TILE) break;
-    if (j > 0 && o > start && o > hold(a.offsets[j - 1], a.tokens)) ends[o - 1 - start] = (int32_t)j;
+    if (o > start && o > before) {   // the sequence j - 1 is not empty: its last token is o - 1
+      const int at = (int)(o - 1 - start);
+      ends.last[at] = a.last_value ? a.last_value[j - 1] : 0.f;
+      atomicOr(&ends.bits[at >> 5], 1u << (at & 31));
+    }
   }
   __syncthreads();
+  t.end = ends.bits[threadIdx.x >> 2] >> (threadIdx.x & 3) * 8 & 0xff;
 #pragma unroll
-  for (int k = 0; k < GAE_PER; ++k) {
-    t.end[k] = ends[threadIdx.x * GAE_PER + k];
-    t.in |= (uint32_t)(i + k >= first && i + k < last) << k;
-  }
-  t.on &= t.in;
+  for (int k = 0; k < GAE_PER; ++k) t.last[k] = ends.last[threadIdx.x * GAE_PER + k];   // used where the bit is set
+  const int64_t lo = first - i, hi = last - i;   // this thread's tokens that lie in a sequence
+  const int l = lo < 0 ? 0 : lo > 8 ? 8 : (int)lo, h = hi < 0 ? 0 : hi > 8 ? 8 : (int)hi;
+  t.on &= ((1u << h) - 1) & ~((1u << l) - 1);
   return offset;
 }
-__device__ __forceinline__ double gae_last(const GaeArgs& a, int32_t end) { return a.last_value ? (double)a.last_value[end - 1] : 0.0; }
 // whether a thread's tokens hide what comes from behind, and the value in front of them then
-__device__ __forceinline__ bool gae_front(const GaeArgs& a, const GaeTile& t, double* v) {
-  bool set = false;
+__device__ __forceinline__ bool gae_front(const GaeTile& t, double* v) {
+  float f = 0.f;
 #pragma unroll
-  for (int k = GAE_PER - 1; k >= 0; --k) {
-    if (t.end[k]) { set = true; *v = gae_last(a, t.end[k]); }
-    if (t.on >> k & 1) { set = true; *v = t.v[k]; }
-  }
-  return set;
+  for (int k = GAE_PER - 1; k >= 0; --k) f = t.on >> k & 1 ? t.v[k] : t.end >> k & 1 ? t.last[k] : f;
+  *v = f;
+  return (t.on | t.end) != 0;
 }
 // what a thread's tokens do to A, V being what enters them
 __device__ __forceinline__ Affine gae_map(const GaeArgs& a, const GaeTile& t, double V) {
@@ -325,18 +338,17 @@ __device__ __forceinline__ Affine gae_map(const GaeArgs& a, const GaeTile& t, do
   const double gl = a.gamma * a.lambda;
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) {
-    if (t.end[k]) { m = Affine{0.0, 0.0}; V = gae_last(a, t.end[k]); }
-    if (t.on >> k & 1) {
-      const double v = t.v[k];
-      m = Affine{gl * m.a, gl * m.c + (a.gamma * V + ((double)t.r[k] - v))};
-      V = v;
-    }
+    const bool on = t.on >> k & 1, end = t.end >> k & 1;
+    const double v = t.v[k];
+    if (end) { m = Affine{0.0, 0.0}; V = t.last[k]; }
+    const double c = gl * m.c + (a.gamma * V + ((double)t.r[k] - v));
+    if (on) { m = Affine{gl * m.a, c}; V = v; }
   }
   return m;
 }
 
 __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
-  __shared__ int32_t ends[GAE_TILE];
+  __shared__ GaeEnds ends;
   __shared__ Affine lds[4];
   __shared__ double lds_v[4];
   __shared__ int lds_set[4];
@@ -345,12 +357,10 @@ __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
   GaeTile t;
   const int64_t offset = gae_load(a, blockIdx.x, -1, ends, t);   // with barriers
   double v = 0, front;
-  bool any, stop = false;
-  const bool set = gae_front(a, t, &v);
-#pragma unroll
-  for (int k = 0; k < GAE_PER; ++k) stop |= t.end[k] != 0;
+  bool any;
+  const bool set = gae_front(t, &v);
   if (t.on) atomicAdd(&count, __popc(t.on));
-  if (stop) stops = 1;
+  if (t.end) stops = 1;
   const double V = block_value<4>(set, v, 0.0, lds_v, lds_set, &front, &any);
   Affine whole;
   block_behind<4>(gae_map(a, t, V), lds, &whole);
@@ -391,7 +401,7 @@ __global__ __launch_bounds__(1024) void k_gae_tiles(GaeArgs a) {
 }
 
 __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
-  __shared__ int32_t ends[GAE_TILE];
+  __shared__ GaeEnds ends;
   __shared__ Affine lds[2][4];
   __shared__ double lds_v[2][4];
   __shared__ int lds_set[2][4];
@@ -417,25 +427,31 @@ __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
   GaeTile t;
   gae_load(a, tile, a.tiles > 1 ? a.map[tile].offset : -1, ends, t);
   double v = 0;
-  const bool set = gae_front(a, t, &v);
+  const bool set = gae_front(t, &v);
   double V = block_value<4>(set, v, in.y, lds_v[0], lds_set[0], nullptr, nullptr);
   double A = apply(block_behind<4>(gae_map(a, t, V), lds[0], nullptr), in.x);
   const double gl = a.gamma * a.lambda;
   float adv[GAE_PER], ret[GAE_PER];
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) {
-    if (t.end[k]) { A = 0; V = gae_last(a, t.end[k]); }
-    const bool on = t.on >> k & 1;
+    const bool on = t.on >> k & 1, end = t.end >> k & 1;
     const double v = t.v[k];
-    if (on) { A = gl * A + (a.gamma * V + ((double)t.r[k] - v)); V = v; }
+    if (end) { A = 0; V = t.last[k]; }
+    const double next = gl * A + (a.gamma * V + ((double)t.r[k] - v));
+    if (on) { A = next; V = v; }
     adv[k] = on ? (float)A : 0.f;
     ret[k] = on ? (float)(A + v) : 0.f;
   }
   const int64_t i = tile * GAE_TILE + threadIdx.x * GAE_PER;
+  if (tile * GAE_TILE + GAE_TILE <= a.tokens) {
 #pragma unroll
-  for (int h = 0; h < GAE_PER; h += 4) {
-    const float x[4] = {adv[h], adv[h + 1], adv[h + 2], adv[h + 3]}, y[4] = {ret[h], ret[h + 1], ret[h + 2], ret[h + 3]};
-    store4(a.adv, i + h, a.tokens, x);
-    store4(a.ret, i + h, a.tokens, y);
+    for (int h = 0; h < GAE_PER; h += 4) {
+      *reinterpret_cast<f32x4_any_t*>(a.adv + i + h) = f32x4_any_t{adv[h], adv[h + 1], adv[h + 2], adv[h + 3]};
+      *reinterpret_cast<f32x4_any_t*>(a.ret + i + h) = f32x4_any_t{ret[h], ret[h + 1], ret[h + 2], ret[h + 3]};
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < GAE_PER; ++k)
+      if (i + k < a.tokens) { a.adv[i + k] = adv[k]; a.ret[i + k] = ret[k]; }
   }
 }
