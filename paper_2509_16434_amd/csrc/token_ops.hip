@@ -319,19 +319,20 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
   CHECK(check_array("d_offsets", d_offsets, 8, pairs > 0 || tokens > 0));
   CHECK(check_ws(d_ws, ws_bytes, ppo_pair_ws_bytes(pairs, tokens)));
   const PairArgs a = {pairs, tokens, d_logp, d_logp_ref, d_mask, d_offsets, hp->kind, hp->length_mean, hp->beta, hp->label_smoothing, hp->scale,
-                      d_dlogp, d_margin, (PairRecord*)d_ws};
+                      d_dlogp, d_margin, pairs > PAIRS_INLINE ? (PairRecord*)d_ws : nullptr, d_stats};
   hipStream_t st = (hipStream_t)hip_stream;
-  const PairGrid g = {pair_slices(pairs, tokens), (double2*)(a.record + pairs)};
+  const PairGrid g = {pair_slices(pairs, tokens), (double2*)((PairRecord*)d_ws + pairs)};
   const int64_t items = 2 * pairs * g.slices;
-  if (pairs == 0 && tokens > 0) hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)std::min<int64_t>(cdiv(tokens, 256), 1024)), dim3(256), 0, st, a, g);
-  else if (pairs > 0 && (tokens / (2 * pairs) <= 64 || (pairs >= 2048 && tokens / (2 * pairs) <= 512))) {
+  const uint32_t extra = a.record ? 0 : 1;   // the block of the statistics
+  if (pairs > 0 && (tokens / (2 * pairs) <= 64 || (pairs >= 2048 && tokens / (2 * pairs) <= 512))) {
     hipLaunchKernelGGL(k_pair_sums<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
-    hipLaunchKernelGGL(k_pair_loss<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
-  } else if (pairs > 0) {
-    hipLaunchKernelGGL(k_pair_sums<256>, dim3((uint32_t)items), dim3(256), 0, st, a, g);
-    hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)items), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL(k_pair_loss<64>, dim3((uint32_t)cdiv(items, 4) + extra), dim3(256), 0, st, a, g);
+  } else {
+    if (pairs > 0) hipLaunchKernelGGL(k_pair_sums<256>, dim3((uint32_t)items), dim3(256), 0, st, a, g);
+    const int64_t blocks = pairs > 0 ? items : std::min<int64_t>(cdiv(tokens, 256), 1024);   // no pairs: the gradient is zeros
+    hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)blocks + extra), dim3(256), 0, st, a, g);
   }
-  hipLaunchKernelGGL(k_pair_stats, dim3(1), dim3(1024), 0, st, pairs, (const PairRecord*)d_ws, hp->scale, d_stats);
+  if (a.record) hipLaunchKernelGGL(k_pair_stats, dim3(1), dim3(1024), 0, st, pairs, (const PairRecord*)a.record, hp->scale, d_stats);
   LAUNCHCHK("the kernels of ppo_pair_loss");
   return PPO_OK;
 }

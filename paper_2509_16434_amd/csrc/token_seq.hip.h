@@ -17,7 +17,8 @@ struct PairArgs {
   int32_t kind, mean;
   float beta, smoothing, scale;
   float *dlogp, *margin;
-  struct PairRecord* record;
+  struct PairRecord* record; // [pairs]; NULL: k_pair_loss finishes the statistics by itself
+  float* stats;
 };
 struct PairRecord { double loss, right, margin, chosen, rejected, active; };
 
@@ -110,11 +111,57 @@ __device__ __forceinline__ double2 pair_sum(const PairGrid& g, int64_t s) {
   return make_double2(lanes_sum<64>(v), lanes_sum<64>(n));
 }
 
-// Gradient (and record) of the pairs.
+__device__ __forceinline__ PairRecord pair_record(const PairArgs& a, const double (&S)[2], bool on) {
+  const double b = a.beta, D = S[0] - S[1];
+  if (!on) return PairRecord{0, 0, 0, 0, 0, 0};
+  return PairRecord{pair_value(a.kind, b, a.smoothing, D), D > 0 ? 1.0 : 0.0, b * D, b * S[0], b * S[1], 1.0};
+}
+// stats: loss, share of pairs with D > 0, mean margin, mean chosen and rejected reward, active pairs, non-finite
+__device__ __forceinline__ void write_pair_stats(const double (&v)[6], float scale, float* stats) {
+  const double n = v[5] > 0 ? v[5] : 1;
+  stats[0] = (float)(v[0] * scale);
+  for (int k = 1; k < 5; ++k) stats[k] = (float)(v[k] / n);
+  stats[5] = (float)v[5];
+  stats[6] = isfinite(stats[0]) ? 0.f : 1.f;
+}
+// The statistics (and margins) of at most PAIRS_INLINE pairs by one block: L lanes per sequence add up its slices' sums, then a thread
+// does a pair.  Saves a launch where launches are what a call costs.
+constexpr int PAIRS_INLINE = 256;
+__device__ __forceinline__ void pair_stats_block(const PairArgs& a, const PairGrid& g) {
+  __shared__ double2 sum[2 * PAIRS_INLINE];
+  __shared__ double lds[6 * 4];
+  const int n = 2 * (int)a.pairs;
+  int L = 64;
+  while (L > 1 && L * n > 256) L >>= 1;
+  for (int s0 = 0; s0 < n; s0 += 256 / L) {
+    const int s = s0 + (int)threadIdx.x / L;
+    double v = 0, c = 0;
+    if (s < n)
+      for (int k = threadIdx.x & (L - 1); k < g.slices; k += L) { const double2 p = g.part[(int64_t)s * g.slices + k]; v += p.x; c += p.y; }
+    for (int o = L >> 1; o; o >>= 1) { v += __shfl_xor(v, o); c += __shfl_xor(c, o); }
+    if (s < n && (threadIdx.x & (L - 1)) == 0) sum[s] = make_double2(v, c);
+  }
+  __syncthreads();
+  PairRecord r = {0, 0, 0, 0, 0, 0};
+  if ((int)threadIdx.x < a.pairs) {
+    const double2 won = sum[threadIdx.x], lost = sum[threadIdx.x + a.pairs];
+    const bool on = won.y > 0 && lost.y > 0;
+    const double S[2] = {a.mean && on ? won.x / won.y : won.x, a.mean && on ? lost.x / lost.y : lost.x};
+    r = pair_record(a, S, on);
+    if (a.margin) a.margin[threadIdx.x] = (float)r.margin;
+  }
+  double v[6] = {r.loss, r.right, r.margin, r.chosen, r.rejected, r.active};
+  block_sums<4>(v, lds);
+  if (threadIdx.x == 0) write_pair_stats(v, a.scale, a.stats);
+}
+
+// Gradient and records of the pairs; without room for records, one more block does the statistics.
 template <int G>
 __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
+  const int64_t blocks = gridDim.x - (a.record ? 0 : 1);
+  if (blockIdx.x == blocks) { pair_stats_block(a, g); return; }
   const int64_t first = hold(a.offsets[0], a.tokens), last = hold(a.offsets[2 * a.pairs], a.tokens);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < first + (a.tokens - last); i += (int64_t)gridDim.x * 256)
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < first + (a.tokens - last); i += blocks * 256)
     a.dlogp[i < first ? i : last + (i - first)] = 0.f;   // tokens of no sequence
   const int64_t item = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
   if (item >= 2 * a.pairs * g.slices) return;
@@ -142,14 +189,13 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
         if (i + q >= from && i + q < to) a.dlogp[i + q] = d[q];
     }
   }
-  if (s < a.pairs && slice == 0 && threadIdx.x % G == 0) {
-    const double b = a.beta;
-    if (a.margin) a.margin[k] = on ? (float)(b * D) : 0.f;
-    a.record[k] = on ? PairRecord{pair_value(a.kind, a.beta, a.smoothing, D), D > 0 ? 1.0 : 0.0, b * D, b * S[0], b * S[1], 1.0} : PairRecord{0, 0, 0, 0, 0, 0};
+  if (a.record && s < a.pairs && slice == 0 && threadIdx.x % G == 0) {
+    const PairRecord r = pair_record(a, S, on);
+    if (a.margin) a.margin[k] = (float)r.margin;
+    a.record[k] = r;
   }
 }
 
-// stats: loss, share of pairs with D > 0, mean margin, mean chosen and rejected reward, active pairs, non-finite
 __global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRecord* rec, float scale, float* stats) {
   __shared__ double lds[6 * 16];
   double v[6] = {0, 0, 0, 0, 0, 0};
@@ -158,12 +204,7 @@ __global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRe
     v[0] += r.loss; v[1] += r.right; v[2] += r.margin; v[3] += r.chosen; v[4] += r.rejected; v[5] += r.active;
   }
   block_sums<16>(v, lds);
-  if (threadIdx.x) return;
-  const double n = v[5] > 0 ? v[5] : 1;
-  stats[0] = (float)(v[0] * scale);
-  for (int k = 1; k < 5; ++k) stats[k] = (float)(v[k] / n);
-  stats[5] = (float)v[5];
-  stats[6] = isfinite(stats[0]) ? 0.f : 1.f;
+  if (threadIdx.x == 0) write_pair_stats(v, scale, stats);
 }
 
 // ---------------------------------------------------------------- advantages

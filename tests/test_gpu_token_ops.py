@@ -4,6 +4,7 @@ graphs, results in the memory of the inputs.
 
 Tolerances count roundings (u = half a step: fp32 2^-24, bf16 2^-8, fp16 2^-11).  A sum of n positive terms in several running sums that
 are joined in a tree is off by at most (n / 64 + 32) u of its value (64: the smallest number of running sums a row is added up in)."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -297,6 +298,14 @@ def test_no_rows():
     assert L.token_gae(z, z, off, 0.9, 0.9)[0].shape == (0,)
     dlogp, margin, stats = L.pair_loss(z, off)
     assert dlogp.shape == margin.shape == (0,) and stats.tolist() == [0.0] * 7
+    hp = L.PairHParams(0, 0, 0.1, 0.0, 1.0)   # through the C call: nothing but the statistics is there
+    stats.fill_(7.0)
+    torch.cuda.synchronize()
+    assert L._lib.ppo_pair_loss(0, 0, None, None, None, None, C.byref(hp), None, None, stats.data_ptr(), None, 0, None) == 0
+    torch.cuda.synchronize()
+    assert stats.tolist() == [0.0] * 7
+    dlogp, margin, stats = L.pair_loss(torch.full((700,), 3.0, device="cuda"), off)   # tokens, but no pair
+    assert dlogp.tolist() == [0.0] * 700 and stats.tolist() == [0.0] * 7
     # only idle rows
     x, t = torch.randn(3, 5, device="cuda"), torch.full((3,), -1, dtype=torch.int32, device="cuda")
     d, stats, logp = L.token_loss(x, t, x[:, 0].contiguous(), x[:, 1].contiguous(), ent_coef=0.5)
@@ -311,7 +320,7 @@ def cuts(lengths, before=0, behind=0):
 
 
 PAIR_LENGTHS = [([1], [1]), ([0], [5]), ([3, 0, 64, 1], [2, 0, 65, 1]), ([5000], [1]), ([257, 1000, 31], [513, 2, 4099]), ([1] * 300, [2] * 300), ([100003, 7], [50001, 9]),
-                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1)))]
+                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1))), ([5] * 256, [3] * 256), ([5] * 257, [3] * 257), ([700] * 130, [90] * 130), ([6000] * 20, [9000] * 20)]
 
 
 def pair_definition(logp, ref, keep, off, pairs, kind, beta, ls, mean, scale):
