@@ -257,6 +257,7 @@ int ppo_forward(ppo_ctx* ctx, const int32_t* d_idx, int64_t count, float* d_mu, 
  * read nor written.  Arrays need the alignment of their element type only.
  * --------------------------------------------------------------------------------------------------------------- */
 #define PPO_TOKEN_MAX_VOCAB (1 << 24)
+#define PPO_TOKEN_MAX_ROWS ((1 << 24) - 1) /* rows of one call; half as many pairs */
 
 /* Dropout whose mask is a function of (seed, layer, row id, column) and is never stored, so that the pass that collects
  * a rollout, every later pass over the same samples in any order, and the backward pass drop the same units:
@@ -293,7 +294,7 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
 typedef struct {
   float temperature;      /* > 0 */
   float clip_lo, clip_hi; /* >= 0; clip_lo <= 1 */
-  float kl_coef;          /* >= 0; without d_logp_ref it must be 0 */
+  float kl_coef;          /* >= 0; without d_logp_ref it must be 0.  0 with one: the estimate is reported only */
   float ent_coef;         /* 0: the entropy is neither computed nor reported */
   float scale;            /* e.g. 1 / number of tokens; a loss scale for fp16 gradients */
 } ppo_token_hparams;
@@ -309,7 +310,8 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
 /* Sequences of the calls below are packed one behind the other: sequence k holds the tokens [d_offsets[k], d_offsets[k+1])
  * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty).  Offsets outside [0, tokens] are taken as its
  * nearer end, and of decreasing ones the results are unspecified; no memory outside the arrays is touched either way.
- * d_mask: uint8 [tokens], 0 = the token is passed over (a prompt, a tool's answer) and its inputs are not read; NULL: none.
+ * d_mask: uint8 [tokens], 0 = the token is passed over (a prompt, a tool's answer) and its inputs may be anything; NULL: none.
+ * (Tokens whose row was idle in ppo_token_logp, with a log-probability of 0, belong there.)
  *
  * Preference loss on `pairs` pairs of sequences, k chosen and pairs + k rejected, from the tokens' log-probabilities.
  * S = sum (logp - logp_ref) over a sequence's unmasked tokens (their mean if length_mean), D = S_chosen - S_rejected:

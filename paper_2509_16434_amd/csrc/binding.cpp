@@ -205,13 +205,18 @@ at::Tensor out_matrix(PyObject* o, const at::Tensor& like) {
   if (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type()) throw Wrong{PyExc_ValueError, "out: expected the shape and type of the input"};
   return t;
 }
-// Memory of `out` and of an input: apart, or the same place with the same row stride.
+// Memory of `out` and of an input: apart, the same place with the same row stride, or side by side in rows of one stride.
 void apart_or_same(const at::Tensor& out, int64_t ldo, const at::Tensor& in, int64_t ldi, const char* name) {
   if (!in.defined() || !out.numel()) return;
   const int64_t es = out.element_size(), rows = out.size(0), cols = out.size(1);
   const char *a = (const char*)out.data_ptr(), *b = (const char*)in.data_ptr();
   const char *ae = a + ((rows - 1) * ldo + cols) * es, *be = b + ((rows - 1) * ldi + cols) * es;
-  if (a < be && b < ae && !(a == b && ldo == ldi)) throw Wrong{PyExc_ValueError, std::string("out overlaps ") + name + " without being it"};
+  if (a >= be || b >= ae || (a == b && ldo == ldi)) return;
+  if (ldo == ldi && (a - b) % es == 0) {
+    const int64_t d = (((a - b) / es) % ldo + ldo) % ldo;
+    if (d >= cols && ldo - d >= cols) return;
+  }
+  throw Wrong{PyExc_ValueError, std::string("out overlaps ") + name + " without being it"};
 }
 template <class T> T* ptr(const at::Tensor& t) { return t.defined() ? (T*)t.data_ptr() : nullptr; }
 PyObject* wrap(at::Tensor t) {

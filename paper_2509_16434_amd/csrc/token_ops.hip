@@ -31,8 +31,10 @@ int fail(int code, const char* fmt, ...) {
     if (e_ != hipSuccess) return fail(PPO_EHIP, "launch of %s failed: %s", what, hipGetErrorString(e_));           \
   } while (0)
 
-constexpr int64_t MAX_ROWS = (int64_t)1 << 30;   // rows, pairs or sequences of one call
-constexpr int64_t MAX_TOKENS = (int64_t)1 << 40;
+constexpr int64_t MAX_ROWS = PPO_TOKEN_MAX_ROWS;      // 256 threads each are a grid of fewer than 2^32; the wider groups belong to rows so
+                                                      // long that memory holds too few of them
+constexpr int64_t MAX_PAIRS = PPO_TOKEN_MAX_ROWS / 2;
+constexpr int64_t MAX_COLS = (int64_t)1 << 30, MAX_SEQUENCES = (int64_t)1 << 30, MAX_TOKENS = (int64_t)1 << 40;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool finite_in(double v, double lo, double hi) { return v >= lo && v <= hi; }
@@ -151,7 +153,8 @@ extern "C" {
 int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int64_t ld_x, const int64_t* d_row_ids, const void* d_residual,
                 int64_t ld_residual, double p, uint64_t seed, uint64_t layer, void* d_y, int64_t ld_y, void* hip_stream) {
   if (dtype < 0 || dtype > 2) return fail(PPO_EINVAL, "dtype must be 0 (fp32), 1 (bf16) or 2 (fp16)");
-  if (rows < 0 || cols < 0 || rows > MAX_ROWS || cols > MAX_ROWS) return fail(PPO_ESHAPE, "rows and columns must be in [0, %lld]", (long long)MAX_ROWS);
+  if (rows < 0 || rows > MAX_ROWS) return fail(PPO_ESHAPE, "rows must be in [0, %lld] (got %lld)", (long long)MAX_ROWS, (long long)rows);
+  if (cols < 0 || cols > MAX_COLS) return fail(PPO_ESHAPE, "columns must be in [0, %lld] (got %lld)", (long long)MAX_COLS, (long long)cols);
   if (!finite_in(p, 0, 1)) return fail(PPO_EINVAL, "p must be in [0, 1]");
   if (rows == 0 || cols == 0) return PPO_OK;
   CHECK(check_rows("d_x", d_x, dtype, cols, ld_x));
@@ -299,13 +302,13 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
 }
 
 int64_t ppo_pair_ws_bytes(int64_t pairs, int64_t tokens) {
-  if (pairs < 0 || pairs > MAX_ROWS / 2 || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
+  if (pairs < 0 || pairs > MAX_PAIRS || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
   return pairs * (int64_t)sizeof(PairRecord) + 2 * pairs * pair_slices(pairs, tokens) * (int64_t)sizeof(double2);
 }
 
 int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const float* d_logp_ref, const uint8_t* d_mask, const int64_t* d_offsets,
                   const ppo_pair_hparams* hp, float* d_dlogp, float* d_margin, float* d_stats, void* d_ws, int64_t ws_bytes, void* hip_stream) {
-  if (pairs < 0 || pairs > MAX_ROWS / 2 || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "pairs or tokens out of range");
+  if (pairs < 0 || pairs > MAX_PAIRS || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "pairs or tokens out of range");
   if (!hp) return fail(PPO_EINVAL, "hp is NULL");
   if (hp->kind < 0 || hp->kind > 1) return fail(PPO_EINVAL, "kind must be 0 (sigmoid) or 1 (squared)");
   if (!(hp->beta > 0) || !isfinite(hp->beta)) return fail(PPO_EINVAL, "beta must be finite and > 0");
@@ -338,14 +341,14 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
 }
 
 int64_t ppo_token_gae_ws_bytes(int64_t sequences, int64_t tokens) {
-  if (sequences < 0 || sequences > MAX_ROWS || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
+  if (sequences < 0 || sequences > MAX_SEQUENCES || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
   const int64_t tiles = gae_tiles(tokens);
   return tiles <= 1 ? 0 : tiles * (int64_t)sizeof(GaeMap) + (tiles > GAE_DIRECT ? tiles * (int64_t)sizeof(double2) : 0);
 }
 
 int ppo_token_gae(int64_t sequences, int64_t tokens, const float* d_reward, const float* d_value, const uint8_t* d_mask, const int64_t* d_offsets,
                   const float* d_last_value, double gamma, double lambda, float* d_adv, float* d_ret, void* d_ws, int64_t ws_bytes, void* hip_stream) {
-  if (sequences < 0 || sequences > MAX_ROWS || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "sequences or tokens out of range");
+  if (sequences < 0 || sequences > MAX_SEQUENCES || tokens < 0 || tokens > MAX_TOKENS) return fail(PPO_ESHAPE, "sequences or tokens out of range");
   if (!finite_in(gamma, 0, 1) || !finite_in(lambda, 0, 1)) return fail(PPO_EINVAL, "gamma and lambda must be in [0, 1]");
   if (tokens == 0) return PPO_OK;
   CHECK(check_array("d_reward", d_reward, 4, true));

@@ -281,6 +281,8 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
 
 // ---- loss
 // Terms of the loss at one token and their derivatives by logp (g) and H (h), all without weight.
+// exp d - 1 - d from exp d - 1: a small difference near 0; with exp d infinite (or past all digits of d) it is that
+__device__ __forceinline__ float less_linear(float em, float d) { return d < 80.f ? em - d : em; }
 struct LossTerm { float g, h; LossRecord rec; };
 struct LossIn { float old, ref, adv, w; };
 __device__ __forceinline__ LossIn loss_in(const RowArgs& a, int64_t row) {
@@ -296,13 +298,13 @@ __device__ __forceinline__ LossTerm loss_term(const RowArgs& a, const LossIn& in
   o.g = held ? 0.f : -s1;
   o.rec.kl = 0.f;
   if (a.logp_ref) {
-    const float d = in.ref - logp, ed = expf(d);
-    o.rec.kl = (ed - d - 1.f) * in.w;
-    o.g += a.kl_coef * (1.f - ed);
+    const float d = in.ref - logp, em = expm1f(d);
+    o.rec.kl = less_linear(em, d) * in.w;
+    if (a.kl_coef != 0.f) o.g -= a.kl_coef * em;   // (it may be infinite where it only is reported)
   }
   o.rec.ent = ent * in.w;
   o.h = -a.ent_coef;
-  o.rec.old_kl = (rho - 1.f) - lr;
+  o.rec.old_kl = less_linear(expm1f(lr), lr);
   o.rec.clipped = rho < lo || rho > hi ? 1.f : 0.f;
   o.rec.active = 1.f;
   o.g *= in.w; o.h *= in.w;
@@ -447,7 +449,7 @@ __global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
 constexpr int STATS_ROWS = 4096;   // rows per block (more when there are more than 1024 such blocks)
 __device__ __forceinline__ void write_stats(const double (&v)[6], float kl_coef, float ent_coef, float* stats) {
   // loss, pi, kl, entropy (weighted sums), mean approx_kl, clipped share, active rows, non-finite
-  const double loss = v[0] + (double)kl_coef * v[1] - (double)ent_coef * v[2], n = v[5] > 0 ? v[5] : 1;
+  const double loss = v[0] + (kl_coef != 0.f ? (double)kl_coef * v[1] : 0.0) - (ent_coef != 0.f ? (double)ent_coef * v[2] : 0.0), n = v[5] > 0 ? v[5] : 1;
   stats[0] = (float)loss; stats[1] = (float)v[0]; stats[2] = (float)v[1]; stats[3] = (float)v[2];
   stats[4] = (float)(v[3] / n); stats[5] = (float)(v[4] / n); stats[6] = (float)v[5];
   stats[7] = isfinite((float)loss) ? 0.f : 1.f;

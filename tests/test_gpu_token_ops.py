@@ -71,7 +71,7 @@ def row_tolerance(d, p, at, V):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 63), (7, 64), (129, 65), (64, 256), (17, 1000), (2, 4097), (33, 8192), (9, 16385), (4, 50257), (1, 131075), (700, 33), (2, 262147),
-          (300, 12289), (40, 70001)]
+          (300, 12289), (40, 70001), (9001, 24), (3, 160001)]
 HARD = {"plain": 0, "banned": 1, "lowest": 2}
 
 
@@ -266,6 +266,35 @@ def test_rows_that_are_not_numbers_are_reported():
     assert logp[0].item() == -math.inf and abs(ent[0].item() - math.log(7)) < 1e-5
     back = L.token_logp_backward(y, t, stat, torch.ones(2, device="cuda"), entropy=ent, dentropy=torch.ones(2, device="cuda"))
     assert bool(torch.isfinite(back).all()) and abs(back[0, 3].item() - 1) < 1e-6   # -p + 1 with p = 0
+
+
+def test_a_reference_that_is_only_reported():
+    """kl_coef 0 with a reference, and a target that its mask forbids: the estimate is infinite, the loss and the gradient are not."""
+    x = torch.randn(3, 40, device="cuda", generator=rnd(2))
+    x[1, 4] = -math.inf
+    t, z = torch.full((3,), 4, dtype=torch.int32, device="cuda"), torch.full((3,), -4.0, device="cuda")
+    d, stats, logp = L.token_loss(x, t, z, z, logp_ref=z)
+    assert bool(torch.isfinite(d).all()) and math.isfinite(stats[0].item()) and stats[2].item() == math.inf and stats[7].item() == 0 and logp[1].item() == -math.inf
+    assert torch.equal(d, L.token_loss(x, t, z, z)[0])
+
+
+def test_many_rows():
+    """More rows than a grid's second dimension holds: every row is that of a call on the last rows alone."""
+    rows, V, first = 66001, 1100, 65000
+    x = torch.randn(rows, V, device="cuda", generator=rnd(6))
+    t = torch.randint(0, V, (rows,), device="cuda", generator=rnd(7)).to(torch.int32)
+    g = torch.randn(rows, device="cuda", generator=rnd(8))
+    part = slice(first, None)
+    logp, _, stat = L.token_logp(x, t)
+    d, dd = L.token_logp_backward(x, t, stat, g), L.dropout(x, 0.5, 4)
+    again, _, stat_again = L.token_logp(x[part], t[part])
+    assert torch.equal(logp[part], again) and torch.equal(d[part], L.token_logp_backward(x[part], t[part], stat_again, g[part]))
+    ids = torch.arange(rows, device="cuda")
+    assert torch.equal(dd[part], L.dropout(x[part], 0.5, 4, row_ids=ids[part]))
+    assert float((d.double().sum(1)).abs().max()) < 1e-4   # a gradient by logits adds up to 0
+    for q in (0, 65534, 65535, 65536, rows - 1):
+        want = g[q].double() * ((torch.arange(V, device="cuda") == t[q]).double() - torch.softmax(x[q].double(), 0))
+        assert float((d[q].double() - want).abs().max()) < 1e-5
 
 
 def test_rows_far_apart():
@@ -594,7 +623,11 @@ def test_on_a_side_stream_and_in_graphs(rows, vocab):
 def test_the_binding_refuses():
     x, t, z = torch.zeros(4, 8, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
     off = torch.tensor([0, 2, 4], dtype=torch.int64, device="cuda")
+    wide = torch.randn(4, 20, device="cuda")   # side by side in the same rows is not an overlap
+    want = L.dropout(wide[:, :8], 0.5, 1)
+    assert torch.equal(L.dropout(wide[:, :8], 0.5, 1, out=wide[:, 8:16]), want) and torch.equal(wide[:, 8:16], want)
     wrong = [
+        lambda: L.dropout(wide[:, :8], 0.5, 1, out=wide[:, 7:15]), lambda: L.dropout(wide[:3, :8], 0.5, 1, out=wide[1:, 4:12]),
         lambda: L.token_logp(x.double(), t), lambda: L.token_logp(x[0], t), lambda: L.token_logp(x.t(), t), lambda: L.token_logp(x, t.long()), lambda: L.token_logp(x, t[:3]),
         lambda: L.token_logp(x[:, ::2], t), lambda: L.token_logp(x, t.cpu()), lambda: L.token_loss(x, t, z, z[:2]), lambda: L.token_loss(x, t, z.half(), z),
         lambda: L.token_loss(x, t, z, z, out=x.half()), lambda: L.token_loss(x, t, z, z, out=x[:3]), lambda: L.token_logp_backward(x, t, z, z),

@@ -24,11 +24,11 @@ def _struct(name, before):
 def test_structs_match_the_header():
     assert _struct("ppo_token_hparams", None) == [f for f, _ in L.TokenHParams._fields_] and C.sizeof(L.TokenHParams) == 24
     assert _struct("ppo_pair_hparams", None) == [f for f, _ in L.PairHParams._fields_] and C.sizeof(L.PairHParams) == 20
-    assert "#define PPO_TOKEN_MAX_VOCAB (1 << 24)" in open(HEADER).read()
+    assert "#define PPO_TOKEN_MAX_VOCAB (1 << 24)" in open(HEADER).read() and "#define PPO_TOKEN_MAX_ROWS ((1 << 24) - 1)" in open(HEADER).read()
 
 
 def test_workspace_sizes():
-    for rows, vocab in ((0, 1), (1, 1), (16, 131072), (1 << 20, 256)):
+    for rows, vocab in ((0, 1), (1, 1), (16, 131072), (1 << 20, 256), ((1 << 24) - 1, 2)):
         assert 0 <= lib.ppo_token_ws_bytes(rows, vocab) <= 4096 * rows + (1 << 20)
     assert lib.ppo_token_ws_bytes(-1, 8) == lib.ppo_token_ws_bytes(8, 0) == lib.ppo_token_ws_bytes(8, (1 << 24) + 1) == L.PPO_ESHAPE
     assert lib.ppo_pair_ws_bytes(4, 100) >= 0 and lib.ppo_pair_ws_bytes(-1, 100) == lib.ppo_pair_ws_bytes(1, -1) == L.PPO_ESHAPE
@@ -39,7 +39,7 @@ DROPOUT = dict(dtype=1, rows=4, cols=8, x=P, ldx=8, ids=NUL, res=NUL, ldr=8, p=0
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(dtype=3), L.PPO_EINVAL), (dict(dtype=-1), L.PPO_EINVAL), (dict(rows=-1), L.PPO_ESHAPE), (dict(cols=-1), L.PPO_ESHAPE), (dict(rows=BIG), L.PPO_ESHAPE),
+    (dict(dtype=3), L.PPO_EINVAL), (dict(dtype=-1), L.PPO_EINVAL), (dict(rows=-1), L.PPO_ESHAPE), (dict(cols=-1), L.PPO_ESHAPE), (dict(rows=BIG), L.PPO_ESHAPE), (dict(rows=1 << 24), L.PPO_ESHAPE), (dict(cols=BIG, ldx=BIG, ldy=BIG), L.PPO_ESHAPE),
     (dict(p=-0.1), L.PPO_EINVAL), (dict(p=1.1), L.PPO_EINVAL), (dict(p=NAN), L.PPO_EINVAL), (dict(x=NUL), L.PPO_EINVAL), (dict(y=NUL), L.PPO_EINVAL),
     (dict(x=ODD), L.PPO_EINVAL), (dict(ldx=7), L.PPO_ESHAPE), (dict(ldy=7), L.PPO_ESHAPE), (dict(res=P, ldr=7), L.PPO_ESHAPE), (dict(ids=P + 4), L.PPO_EINVAL),
     (dict(rows=0, x=NUL, y=NUL), 0), (dict(cols=0, x=NUL, y=NUL), 0),
@@ -55,7 +55,7 @@ LOGP = dict(dtype=1, rows=4, vocab=8, x=P, ld=8, target=P, temperature=1.0, logp
 
 
 @pytest.mark.parametrize("change,code", [
-    (dict(dtype=5), L.PPO_EINVAL), (dict(rows=-1), L.PPO_ESHAPE), (dict(vocab=0), L.PPO_ESHAPE), (dict(vocab=(1 << 24) + 1, ld=1 << 25), L.PPO_ESHAPE),
+    (dict(dtype=5), L.PPO_EINVAL), (dict(rows=-1), L.PPO_ESHAPE), (dict(rows=1 << 24), L.PPO_ESHAPE), (dict(vocab=0), L.PPO_ESHAPE), (dict(vocab=(1 << 24) + 1, ld=1 << 25), L.PPO_ESHAPE),
     (dict(temperature=0.0), L.PPO_EINVAL), (dict(temperature=-1.0), L.PPO_EINVAL), (dict(temperature=INF), L.PPO_EINVAL), (dict(temperature=NAN), L.PPO_EINVAL),
     (dict(temperature=1e-45), L.PPO_EINVAL), (dict(x=NUL), L.PPO_EINVAL), (dict(x=ODD), L.PPO_EINVAL), (dict(ld=7), L.PPO_ESHAPE), (dict(target=NUL), L.PPO_EINVAL),
     (dict(logp=NUL), L.PPO_EINVAL), (dict(stat=P + 2), L.PPO_EINVAL), (dict(rows=0, x=NUL, target=NUL, logp=NUL, ws=NUL, wsb=0), 0),
@@ -100,7 +100,7 @@ PHP = dict(kind=0, length_mean=0, beta=0.1, label_smoothing=0.0, scale=1.0)
 
 
 @pytest.mark.parametrize("change,hp,code", [
-    (dict(pairs=-1), {}, L.PPO_ESHAPE), (dict(tokens=-1), {}, L.PPO_ESHAPE), (dict(hp=0), {}, L.PPO_EINVAL), ({}, dict(kind=2), L.PPO_EINVAL), ({}, dict(kind=-1), L.PPO_EINVAL),
+    (dict(pairs=-1), {}, L.PPO_ESHAPE), (dict(pairs=1 << 23), {}, L.PPO_ESHAPE), (dict(tokens=-1), {}, L.PPO_ESHAPE), (dict(hp=0), {}, L.PPO_EINVAL), ({}, dict(kind=2), L.PPO_EINVAL), ({}, dict(kind=-1), L.PPO_EINVAL),
     ({}, dict(beta=0.0), L.PPO_EINVAL), ({}, dict(beta=INF), L.PPO_EINVAL), ({}, dict(label_smoothing=1.5), L.PPO_EINVAL), ({}, dict(label_smoothing=NAN), L.PPO_EINVAL),
     ({}, dict(scale=NAN), L.PPO_EINVAL), (dict(logp=NUL), {}, L.PPO_EINVAL), (dict(dlogp=NUL), {}, L.PPO_EINVAL), (dict(offsets=NUL), {}, L.PPO_EINVAL),
     (dict(offsets=P + 4), {}, L.PPO_EINVAL), (dict(stats=NUL), {}, L.PPO_EINVAL), (dict(ws=NUL), {}, L.PPO_EINVAL), (dict(wsb=4), {}, L.PPO_EINVAL), (dict(ref=P + 1), {}, L.PPO_EINVAL),
