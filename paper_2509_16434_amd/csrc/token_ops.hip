@@ -117,7 +117,8 @@ void with_flag(bool on, F f) {
   else f(std::false_type());
 }
 
-// The kernel of a loss: the narrowest group whose registers hold the row.
+// The kernel of a loss: the narrowest group whose registers hold the row; four rows a wave (16 threads each) are 131072 rows of 257 in
+// 48 us where one is 86, but fewer and longer chains for few rows (448 of 256: 4.9 and 3.4 us).
 template <class T, bool ENT>
 void launch_loss(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = cdiv(a.vocab, Piece<T>::N);
@@ -132,8 +133,12 @@ void launch_loss(const RowArgs& a, hipStream_t st) {
     return;                                                                                                                                   \
   }
   LOSS(16, 2)
-  LOSS(64, 1)
-  LOSS(64, 2)
+  if (a.rows < 4096) {
+    LOSS(64, 1)
+    LOSS(64, 2)
+  }
+  LOSS(16, 4)
+  LOSS(16, 8)
   LOSS(64, 4)
   LOSS(64, 8)
   LOSS(256, 4)
@@ -141,7 +146,7 @@ void launch_loss(const RowArgs& a, hipStream_t st) {
   LOSS(256, 16)
   LOSS(512, 16)
   LOSS(1024, 16)
-  LOSS(1024, 24)
+  LOSS(1024, 25)
 #undef LOSS
   hipLaunchKernelGGL((k_token_loss_long<T, ENT>), dim3((uint32_t)a.rows), dim3(1024), 0, st, a);
 }
@@ -212,7 +217,7 @@ int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
       if (a.slices > 1) {
         hipLaunchKernelGGL((k_token_part<T, ENT>), dim3(a.slices, (uint32_t)rows), dim3(256), 0, st, a);
         hipLaunchKernelGGL(k_token_join<ENT>, dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
-      } else if (pieces <= 32) hipLaunchKernelGGL((k_token_logp<T, 16, ENT>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
+      } else if (pieces <= 128) hipLaunchKernelGGL((k_token_logp<T, 16, ENT>), dim3((uint32_t)cdiv(rows, 16)), dim3(256), 0, st, a);
       else if (pieces <= 512) hipLaunchKernelGGL((k_token_logp<T, 64, ENT>), dim3((uint32_t)cdiv(rows, 4)), dim3(256), 0, st, a);
       else hipLaunchKernelGGL((k_token_logp<T, 256, ENT>), dim3((uint32_t)rows), dim3(256), 0, st, a);
     });
@@ -303,7 +308,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
 
 int64_t ppo_pair_ws_bytes(int64_t pairs, int64_t tokens) {
   if (pairs < 0 || pairs > MAX_PAIRS || tokens < 0 || tokens > MAX_TOKENS) return PPO_ESHAPE;
-  return pairs * (int64_t)sizeof(PairRecord) + 2 * pairs * pair_slices(pairs, tokens) * (int64_t)sizeof(double2);
+  return pairs * (int64_t)sizeof(PairRecord) + 2 * pairs * pair_slices(pairs, tokens) * (int64_t)sizeof(double2) + (stats_blocks(pairs) > 1 ? stats_blocks(pairs) * 48 : 0);
 }
 
 int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const float* d_logp_ref, const uint8_t* d_mask, const int64_t* d_offsets,
@@ -327,7 +332,11 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
   const PairGrid g = {pair_slices(pairs, tokens), (double2*)((PairRecord*)d_ws + pairs)};
   const int64_t items = 2 * pairs * g.slices;
   const uint32_t extra = a.record ? 0 : 1;   // the block of the statistics
-  if (pairs > 0 && (tokens / (2 * pairs) <= 64 || (pairs >= 2048 && tokens / (2 * pairs) <= 512))) {
+  const int64_t mean = pairs > 0 ? tokens / (2 * pairs) : 0;
+  if (pairs > 0 && mean <= 64) {
+    hipLaunchKernelGGL(k_pair_sums<16>, dim3((uint32_t)cdiv(items, 16)), dim3(256), 0, st, a, g);
+    hipLaunchKernelGGL(k_pair_loss<16>, dim3((uint32_t)cdiv(items, 16) + extra), dim3(256), 0, st, a, g);
+  } else if (pairs >= 2048 && mean <= 512) {
     hipLaunchKernelGGL(k_pair_sums<64>, dim3((uint32_t)cdiv(items, 4)), dim3(256), 0, st, a, g);
     hipLaunchKernelGGL(k_pair_loss<64>, dim3((uint32_t)cdiv(items, 4) + extra), dim3(256), 0, st, a, g);
   } else {
@@ -335,7 +344,12 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
     const int64_t blocks = pairs > 0 ? items : std::min<int64_t>(cdiv(tokens, 256), 1024);   // no pairs: the gradient is zeros
     hipLaunchKernelGGL(k_pair_loss<256>, dim3((uint32_t)blocks + extra), dim3(256), 0, st, a, g);
   }
-  if (a.record) hipLaunchKernelGGL(k_pair_stats, dim3(1), dim3(1024), 0, st, pairs, (const PairRecord*)a.record, hp->scale, d_stats);
+  if (a.record) {
+    const int blocks = stats_blocks(pairs);
+    double* part = (double*)(g.part + items);
+    hipLaunchKernelGGL(k_pair_stats, dim3(blocks), dim3(1024), 0, st, pairs, cdiv(pairs, blocks), (const PairRecord*)a.record, hp->scale, d_stats, part);
+    if (blocks > 1) hipLaunchKernelGGL(k_pair_stats_join, dim3(1), dim3(1024), 0, st, blocks, hp->scale, d_stats, (const double*)part);
+  }
   LAUNCHCHK("the kernels of ppo_pair_loss");
   return PPO_OK;
 }

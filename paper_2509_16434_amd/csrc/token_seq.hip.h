@@ -33,7 +33,7 @@ __device__ __forceinline__ double pair_slope(int kind, double beta, double ls, d
 }
 
 // What a launch of the two kernels below knows of the grid: a sequence is worked on by `slices` groups of G threads, four tokens a
-// thread at a time; a group per wave (G = 64) for short sequences, per block (G = 256) for long ones.
+// thread at a time; G = 16 or 64 threads for many short sequences (200000 of 10 tokens: 156 us by waves), blocks for long ones.
 struct PairGrid {
   int32_t slices;
   double2* part;       // [2 * pairs][slices]: sum of an unmasked sequence's terms, and how many
@@ -77,8 +77,8 @@ template <int G>
 __global__ __launch_bounds__(256) void k_pair_sums(PairArgs a, PairGrid g) {
   __shared__ double lds[8];
   const int64_t item = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;   // a sequence's slice
-  if (G == 64 && item >= 2 * a.pairs * g.slices) return;
-  const int64_t s = item / g.slices;
+  if (G < 256 && item >= 2 * a.pairs * g.slices) return;
+  const int64_t s = g.slices == 1 ? item : item / g.slices;
   const int slice = (int)(item - s * g.slices);
   const int64_t from = hold(a.offsets[s], a.tokens), to = hold(a.offsets[s + 1], a.tokens);
   double v = 0;
@@ -99,7 +99,8 @@ __global__ __launch_bounds__(256) void k_pair_sums(PairArgs a, PairGrid g) {
     }
   }
   double sums[2] = {v, (double)c};
-  block_sums<G / 64>(sums, lds);
+  if constexpr (G < 64) { sums[0] = lanes_sum<G>(sums[0]); sums[1] = lanes_sum<G>(sums[1]); }
+  else block_sums<G / 64>(sums, lds);
   if (threadIdx.x % G == 0) g.part[item] = make_double2(sums[0], sums[1]);
 }
 
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
     a.dlogp[i < first ? i : last + (i - first)] = 0.f;   // tokens of no sequence
   const int64_t item = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
   if (item >= 2 * a.pairs * g.slices) return;
-  const int64_t s = item / g.slices;
+  const int64_t s = g.slices == 1 ? item : item / g.slices;
   const int slice = (int)(item - s * g.slices);
   const int64_t k = s < a.pairs ? s : s - a.pairs;
   const double2 won = pair_sum(g, k), lost = pair_sum(g, k + a.pairs);
@@ -196,13 +197,25 @@ __global__ __launch_bounds__(256) void k_pair_loss(PairArgs a, PairGrid g) {
   }
 }
 
-__global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, const PairRecord* rec, float scale, float* stats) {
+// More pairs: their records, `share` of them per block; several blocks leave their sums for k_pair_stats_join.
+__global__ __launch_bounds__(1024) void k_pair_stats(int64_t pairs, int64_t share, const PairRecord* rec, float scale, float* stats, double* part) {
   __shared__ double lds[6 * 16];
   double v[6] = {0, 0, 0, 0, 0, 0};
-  for (int64_t i = threadIdx.x; i < pairs; i += 1024) {
+  const int64_t from = blockIdx.x * share, to = from + share < pairs ? from + share : pairs;
+  for (int64_t i = from + threadIdx.x; i < to; i += 1024) {
     const PairRecord r = rec[i];
     v[0] += r.loss; v[1] += r.right; v[2] += r.margin; v[3] += r.chosen; v[4] += r.rejected; v[5] += r.active;
   }
+  block_sums<16>(v, lds);
+  if (threadIdx.x) return;
+  if (gridDim.x == 1) write_pair_stats(v, scale, stats);
+  else
+    for (int k = 0; k < 6; ++k) part[6 * blockIdx.x + k] = v[k];
+}
+__global__ __launch_bounds__(1024) void k_pair_stats_join(int blocks, float scale, float* stats, const double* part) {
+  __shared__ double lds[6 * 16];
+  double v[6];
+  for (int k = 0; k < 6; ++k) v[k] = (int)threadIdx.x < blocks ? part[6 * threadIdx.x + k] : 0.0;
   block_sums<16>(v, lds);
   if (threadIdx.x == 0) write_pair_stats(v, scale, stats);
 }

@@ -71,7 +71,7 @@ def row_tolerance(d, p, at, V):
 
 
 SHAPES = [(1, 1), (3, 2), (5, 63), (7, 64), (129, 65), (64, 256), (17, 1000), (2, 4097), (33, 8192), (9, 16385), (4, 50257), (1, 131075), (700, 33), (2, 262147),
-          (300, 12289), (40, 70001), (9001, 24), (3, 160001)]
+          (300, 12289), (40, 70001), (9001, 24), (3, 160001), (50, 300), (50, 700), (2, 204803)]
 HARD = {"plain": 0, "banned": 1, "lowest": 2}
 
 
@@ -349,7 +349,7 @@ def cuts(lengths, before=0, behind=0):
 
 
 PAIR_LENGTHS = [([1], [1]), ([0], [5]), ([3, 0, 64, 1], [2, 0, 65, 1]), ([5000], [1]), ([257, 1000, 31], [513, 2, 4099]), ([1] * 300, [2] * 300), ([100003, 7], [50001, 9]),
-                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1))), ([5] * 256, [3] * 256), ([5] * 257, [3] * 257), ([700] * 130, [90] * 130), ([6000] * 20, [9000] * 20)]
+                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1))), ([5] * 256, [3] * 256), ([5] * 257, [3] * 257), ([700] * 130, [90] * 130), ([6000] * 20, [9000] * 20), ([2] * 5000, [1] * 5000)]
 
 
 def pair_definition(logp, ref, keep, off, pairs, kind, beta, ls, mean, scale):
