@@ -308,7 +308,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
                    int64_t ws_bytes, void* hip_stream);
 
 /* Sequences of the calls below are packed one behind the other: sequence k holds the tokens [d_offsets[k], d_offsets[k+1])
- * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty).  Offsets outside [0, tokens] are taken as its
+ * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty; tokens <= 2^34).  Offsets outside [0, tokens] are taken as its
  * nearer end, and of decreasing ones the results are unspecified; no memory outside the arrays is touched either way.
  * d_mask: uint8 [tokens], 0 = the token is passed over (a prompt, a tool's answer) and its inputs may be anything; NULL: none.
  * (Tokens whose row was idle in ppo_token_logp, with a log-probability of 0, belong there.)

@@ -34,7 +34,7 @@ int fail(int code, const char* fmt, ...) {
 constexpr int64_t MAX_ROWS = PPO_TOKEN_MAX_ROWS;      // 256 threads each are a grid of fewer than 2^32; the wider groups belong to rows so
                                                       // long that memory holds too few of them
 constexpr int64_t MAX_PAIRS = PPO_TOKEN_MAX_ROWS / 2;
-constexpr int64_t MAX_COLS = (int64_t)1 << 30, MAX_SEQUENCES = (int64_t)1 << 30, MAX_TOKENS = (int64_t)1 << 40;
+constexpr int64_t MAX_COLS = (int64_t)1 << 30, MAX_STRIDE = (int64_t)1 << 40, MAX_SEQUENCES = (int64_t)1 << 30, MAX_TOKENS = (int64_t)1 << 34;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool finite_in(double v, double lo, double hi) { return v >= lo && v <= hi; }
@@ -45,7 +45,7 @@ int elem_bytes(int32_t dtype) { return dtype == 0 ? 4 : 2; }
 int check_rows(const char* name, const void* p, int32_t dtype, int64_t cols, int64_t ld) {
   if (!p) return fail(PPO_EINVAL, "%s is NULL", name);
   if (!aligned(p, elem_bytes(dtype))) return fail(PPO_EINVAL, "%s is not aligned to its element type", name);
-  if (ld < cols || ld > MAX_TOKENS) return fail(PPO_ESHAPE, "%s: row stride %lld does not hold rows of %lld", name, (long long)ld, (long long)cols);
+  if (ld < cols || ld > MAX_STRIDE) return fail(PPO_ESHAPE, "%s: row stride %lld does not hold rows of %lld", name, (long long)ld, (long long)cols);
   return PPO_OK;
 }
 int check_array(const char* name, const void* p, int bytes, bool needed) {
@@ -102,6 +102,7 @@ void with_type(int32_t dtype, F f) {
   else if (dtype == 1) f(bf16_t());
   else f(f16_t());
 }
+
 // Groups of threads per sequence of the preference loss: enough that few long sequences fill the chip, none with less than 1024 tokens
 // on the average.
 int pair_slices(int64_t pairs, int64_t tokens) {
@@ -287,7 +288,6 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / hp->temperature;
   a.logp = d_logp; a.dlogits = d_dlogits; a.logp_old = d_logp_old; a.logp_ref = d_logp_ref; a.adv = d_adv; a.weight = d_weight;
   a.clip_lo = hp->clip_lo; a.clip_hi = hp->clip_hi; a.kl_coef = hp->kl_coef; a.ent_coef = hp->ent_coef; a.scale = hp->scale;
- 
   hipStream_t st = (hipStream_t)hip_stream;
   if (rows > 0) {
     set_slices(a, SLICED_LOSS_ROWS);

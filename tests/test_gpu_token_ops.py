@@ -223,6 +223,10 @@ def test_token_loss(rows, vocab, dtype):
         assert got_stats[6].item() == stats[6]
         there = copy_in_place(x, store)
         assert torch.equal(L.token_loss(there, target, old, adv, logp_ref=use_ref, weight=weight, out=there, **hp)[0], got), "in the logits' own memory, and twice the same"
+        whole = there.new_empty(0).set_(there.untyped_storage()).clone()
+        for m in (whole, store):   # what lies between the rows stays
+            m.as_strided(x.shape, x.stride(), x.storage_offset()).zero_()
+        assert torch.equal(whole.view(torch.uint8), store.view(torch.uint8))
 
 
 def test_token_loss_directional_differences():
@@ -247,17 +251,27 @@ def test_token_loss_directional_differences():
     assert bool((grad[4] == 0).all())
 
 
-def test_rows_that_are_not_numbers_are_reported():
-    x = torch.randn(4, 300, device="cuda", generator=rnd(1))
-    x[1, 7], x[2, 299] = float("nan"), float("inf")
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("vocab", [40, 300, 3000, 9000, 40000, 70000, 140000, 210000])
+def test_rows_that_are_not_numbers_are_reported(vocab, dtype):
+    x = torch.randn(5, vocab, device="cuda", generator=rnd(1)).to(TYPES[dtype])
+    x[1, 7], x[2, vocab - 1] = float("nan"), float("inf")
     x[3] = -math.inf
     x[3, 5] = float("nan")
-    t = torch.zeros(4, dtype=torch.int32, device="cuda")
-    logp, ent, _ = L.token_logp(x, t, want_entropy=True)
-    assert torch.isnan(logp).tolist() == [False, True, True, True] == torch.isnan(ent).tolist()
-    z = torch.zeros(4, device="cuda")
-    d, stats, _ = L.token_loss(x, t, z, z + 1)
-    assert stats[7].item() == 1.0 and bool(torch.isfinite(d[0]).all()) and bool(torch.isnan(d[1]).any())
+    x[4] = -math.inf
+    t = torch.zeros(5, dtype=torch.int32, device="cuda")
+    logp, ent, stat = L.token_logp(x, t, want_entropy=True)
+    assert torch.isnan(logp).tolist() == [False, True, True, True, False] == torch.isnan(ent).tolist()
+    z = torch.zeros(5, device="cuda")
+    for ent_coef in (0.0, 0.1):
+        d, stats, _ = L.token_loss(x, t, z, z + 1, ent_coef=ent_coef)
+        back = L.token_logp_backward(x, t, stat, z + 1, entropy=ent, dentropy=z + ent_coef)
+        assert stats[7].item() == 1.0 and math.isnan(stats[0].item()) and stats[6].item() == 4
+        for grad in (d, back):
+            assert bool(torch.isfinite(grad[0]).all()) and all(bool(torch.isnan(grad[k]).any()) for k in (1, 2, 3)) and not bool(grad[4].any())
+
+
+def test_targets_that_a_mask_forbids():
     # a target that its mask forbids: log-probability -infinity, no NaN elsewhere
     y = torch.zeros(2, 8, device="cuda")
     y[0, 3] = -math.inf
@@ -474,6 +488,25 @@ def test_token_gae(case):
             off_by = np.abs(a.double().cpu().numpy() - b)
             assert (off_by <= U32 * np.abs(b) * 1.01 + 1e-10).all(), (k, off_by.max())
         assert torch.equal(got, L.token_gae(r, v, off, gamma, lam, last_value=last, mask=mask)[0])
+
+
+@pytest.mark.parametrize("lengths", [[3000001], [100000, 2800000, 0, 7], [9000000], [8500000, 400001], [4096] * 2200])
+def test_token_gae_over_many_tiles(lengths):
+    """Long batches, by the recurrence itself: every advantage and its successor's, each rounded once, satisfy it to their roundings; the last
+    tokens give the boundary values."""
+    off, T = cuts(lengths)
+    g = rnd(len(lengths))
+    r, v = 0.1 * torch.randn(T, generator=g, device="cuda"), torch.randn(T, generator=g, device="cuda")
+    last = torch.randn(len(lengths), generator=g, device="cuda")
+    for gamma, lam in ((0.9999, 1.0), (0.99, 0.95)):
+        adv, ret = (x.double() for x in L.token_gae(r, v, off, gamma, lam, last_value=last))
+        nonempty = off[1:] > off[:-1]
+        tails = (off[1:] - 1)[nonempty]
+        after, v_after = torch.cat([adv[1:], adv[:1]]), torch.cat([v[1:], v[:1]]).double()
+        after[tails], v_after[tails] = 0.0, last.double()[nonempty]
+        rest = adv - (r.double() + gamma * v_after - v.double() + gamma * lam * after)
+        assert bool((rest.abs() <= 1.01 * U32 * (adv.abs() + after.abs()) + 1e-10).all())
+        assert bool(((ret - adv - v.double()).abs() <= 1.01 * U32 * (ret.abs() + adv.abs()) + 1e-10).all())
 
 
 def test_token_gae_is_ppo_gae_on_full_sequences():
