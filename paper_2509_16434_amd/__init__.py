@@ -1,6 +1,8 @@
 """MI355X-native PPO learner hot path (experience buffer, GAE, clipped-PPO and
-distillation minibatch updates of a depth-CNN + MLP actor-critic) behind a
-C-ABI HIP library.  `learner` is the thin ctypes binding; `configs` and `synth`
+distillation minibatch updates of a depth-CNN + MLP actor-critic) and operators
+of a policy that answers in tokens (dropout by sample id, token log-probabilities,
+clipped and preference losses, packed advantages) behind a C-ABI HIP library.
+`learner` is the thin binding; `configs` and `synth`
 hold the workload registry and the seeded input generators."""
 from . import configs, synth  # noqa: F401
 

@@ -235,7 +235,7 @@ __global__ __launch_bounds__(1024) void k_pair_stats_join(int blocks, float scal
 // own by itself, and one tile needs nothing else.  A sum over a long sequence (gamma lambda = 1) is held in 64 bits.
 //
 // Bound: 16 to 17 bytes a token, the inputs twice (from the last-level cache the second time) where there is more than one tile:
-// 3 M tokens 12.9 + 14.7 us, 11 at the rate of a copy; 200000 tokens 7.0 + 6.3 us, which is latency.
+// 3 M tokens 10.0 + 15.0 us, 11 at the rate of a copy; 200000 tokens 5.3 + 6.3 us, which is latency.
 constexpr int GAE_PER = 8, GAE_TILE = 256 * GAE_PER;   // tokens per thread and per tile
 constexpr int GAE_DIRECT = 4096;                       // at most so many tiles are scanned directly
 struct GaeMap { double a, b, c; float v; int32_t set, stop, offset; };   // set: V -> v, else V stays; stop: nothing from behind
@@ -249,7 +249,7 @@ struct GaeArgs {
   float *adv, *ret;
   int64_t tiles;
   GaeMap* map;                               // [tiles]
-  double2* in;                               // [tiles] the pair (A, V) that enters a tile; NULL: direct
+  double2* in;                               // [tiles] the pair (A, V) that enters a tile (V a number of 32 bits); NULL: direct
 };
 // A -> a A + c; with a = 0 nothing of A matters, not even NaN: another sequence's is not to be seen
 struct Affine { double a, c; };
@@ -293,15 +293,15 @@ __device__ __forceinline__ Affine block_behind(const Affine& mine, Affine* lds, 
 // The value that enters a thread from behind: that in front of the nearest thread behind it which has one (set), or `in`.  *front, *any:
 // what leaves the block, and whether it is the block's own.  One barrier.
 template <int NW>
-__device__ __forceinline__ double block_value(bool set, double v, double in, double* lds_v, int* lds_set, double* front, bool* any) {
+__device__ __forceinline__ float block_value(bool set, float v, float in, float* lds_v, int* lds_set, float* front, bool* any) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t who = __ballot(set);
   if (set && lane == __ffsll((unsigned long long)who) - 1) lds_v[wave] = v;
   if (lane == 0) lds_set[wave] = who != 0;
   __syncthreads();
   const uint64_t above = lane == 63 ? 0 : who >> (lane + 1);
-  const double near = __shfl(v, above ? lane + __ffsll((unsigned long long)above) : 0);
-  double x = in, out = in;
+  const float near = __shfl(v, above ? lane + __ffsll((unsigned long long)above) : 0);
+  float x = in, out = in;
   bool found = false;
 #pragma unroll 4
   for (int w = NW - 1; w >= 0; --w) {
@@ -353,10 +353,10 @@ __device__ __forceinline__ int64_t gae_load(const GaeArgs& a, int64_t tile, int6
   } else {
 #pragma unroll
     for (int k = 0; k < GAE_PER; ++k) {
-      const bool in = i + k < a.tokens;
-      t.r[k] = in ? a.reward[i + k] : 0.f;
-      t.v[k] = in ? a.value[i + k] : 0.f;
-      t.on |= (uint32_t)(in && (!a.mask || a.mask[i + k])) << k;
+      const int64_t j = i + k < a.tokens ? i + k : a.tokens - 1;   // no branch around a load: they are all in flight together
+      t.r[k] = a.reward[j];
+      t.v[k] = a.value[j];
+      t.on |= (uint32_t)((!a.mask || a.mask[j] != 0) && i + k < a.tokens) << k;
     }
   }
   if (threadIdx.x < GAE_TILE / 32) ends.bits[threadIdx.x] = 0;
@@ -382,60 +382,72 @@ __device__ __forceinline__ int64_t gae_load(const GaeArgs& a, int64_t tile, int6
   return offset;
 }
 // whether a thread's tokens hide what comes from behind, and the value in front of them then
-__device__ __forceinline__ bool gae_front(const GaeTile& t, double* v) {
+__device__ __forceinline__ bool gae_front(const GaeTile& t, float* v) {
   float f = 0.f;
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) f = t.on >> k & 1 ? t.v[k] : t.end >> k & 1 ? t.last[k] : f;
   *v = f;
   return (t.on | t.end) != 0;
 }
-// what a thread's tokens do to A, V being what enters them
-__device__ __forceinline__ Affine gae_map(const GaeArgs& a, const GaeTile& t, double V) {
-  Affine m = {1.0, 0.0};
+// what a thread's tokens do to A, V being the value that enters them; delta: r + gamma V' - V of every token
+__device__ __forceinline__ Affine gae_map(const GaeArgs& a, const GaeTile& t, float V, double (&delta)[GAE_PER]) {
   const double gl = a.gamma * a.lambda;
+  double c = 0;
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) {
     const bool on = t.on >> k & 1, end = t.end >> k & 1;
-    const double v = t.v[k];
-    if (end) { m = Affine{0.0, 0.0}; V = t.last[k]; }
-    const double c = gl * m.c + (a.gamma * V + ((double)t.r[k] - v));
-    if (on) { m = Affine{gl * m.a, c}; V = v; }
+    if (end) { c = 0; V = t.last[k]; }
+    delta[k] = a.gamma * V + ((double)t.r[k] - (double)t.v[k]);
+    if (on) { c = gl * c + delta[k]; V = t.v[k]; }
   }
-  return m;
+  // gamma lambda once for every unmasked token
+  const int n = __popc(t.on);
+  const double g2 = gl * gl, g4 = g2 * g2;
+  double m = n & 1 ? gl : 1.0;
+  if (n & 2) m *= g2;
+  if (n & 4) m *= g4;
+  if (n & 8) m = g4 * g4;
+  return Affine{t.end ? 0.0 : m, c};
 }
 
 __global__ __launch_bounds__(256) void k_gae_part(GaeArgs a) {
   __shared__ GaeEnds ends;
   __shared__ Affine lds[4];
-  __shared__ double lds_v[4];
+  __shared__ float lds_v[4];
   __shared__ int lds_set[4];
-  __shared__ int count, stops;
-  if (threadIdx.x == 0) count = stops = 0;
+  __shared__ int counts[4], ends_in[4];
   GaeTile t;
   const int64_t offset = gae_load(a, blockIdx.x, -1, ends, t);   // with barriers
-  double v = 0, front;
+  float v, front;
   bool any;
   const bool set = gae_front(t, &v);
-  if (t.on) atomicAdd(&count, __popc(t.on));
-  if (t.end) stops = 1;
-  const double V = block_value<4>(set, v, 0.0, lds_v, lds_set, &front, &any);
+  // the tile's unmasked tokens and whether a sequence ends in it, by the waves' ballots (an atomic addition in LDS by every thread costs 4 us
+  // of 13 here)
+  int on = 0;
+#pragma unroll
+  for (int k = 0; k < GAE_PER; ++k) on += __popcll(__ballot(t.on >> k & 1));
+  const bool ends_here = __ballot(t.end != 0) != 0;
+  if ((threadIdx.x & 63) == 0) { counts[threadIdx.x >> 6] = on; ends_in[threadIdx.x >> 6] = ends_here; }
+  const float V = block_value<4>(set, v, 0.f, lds_v, lds_set, &front, &any);
   Affine whole;
-  block_behind<4>(gae_map(a, t, V), lds, &whole);
+  double delta[GAE_PER];
+  block_behind<4>(gae_map(a, t, V, delta), lds, &whole);
   if (threadIdx.x == 0) {
     // without the end of a sequence in the tile, V comes into the last of its n unmasked tokens, and n - 1 more times gamma lambda
     const double gl = a.gamma * a.lambda;
+    const int count = counts[0] + counts[1] + counts[2] + counts[3], stops = ends_in[0] | ends_in[1] | ends_in[2] | ends_in[3];
     const double b = stops || count == 0 ? 0.0 : count == 1 ? a.gamma : gl > 0 ? whole.a / gl * a.gamma : 0.0;
-    a.map[blockIdx.x] = GaeMap{stops ? 0.0 : whole.a, b, whole.c, (float)front, any, stops, (int32_t)offset};
+    a.map[blockIdx.x] = GaeMap{stops ? 0.0 : whole.a, b, whole.c, front, any, stops, (int32_t)offset};
   }
 }
 
 // The pair that leaves a run of tiles at its front, by a block of NW waves, one tile's map a thread (the farthest in the last thread), `far`
 // being the pair that enters the last of them.  The pair that enters this thread's tile goes to *mine.
 template <int NW>
-__device__ __forceinline__ double2 gae_tiles(const GaeMap& m, double2 far, double2* mine, Affine* lds, double* lds_v, int* lds_set) {
-  double front;
+__device__ __forceinline__ double2 gae_tiles(const GaeMap& m, double2 far, double2* mine, Affine* lds, float* lds_v, int* lds_set) {
+  float front;
   bool any;
-  const double V = block_value<NW>(m.set, m.v, far.y, lds_v, lds_set, &front, &any);
+  const float V = block_value<NW>(m.set, m.v, (float)far.y, lds_v, lds_set, &front, &any);
   Affine whole;
   const Affine behind = block_behind<NW>(Affine{m.a, m.b == 0 ? m.c : m.c + m.b * V}, lds, &whole);
   if (mine) *mine = make_double2(apply(behind, far.x), V);
@@ -445,7 +457,7 @@ __device__ __forceinline__ GaeMap gae_nothing() { return GaeMap{1, 0, 0, 0, 0, 0
 
 __global__ __launch_bounds__(1024) void k_gae_tiles(GaeArgs a) {
   __shared__ Affine lds[16];
-  __shared__ double lds_v[16];
+  __shared__ float lds_v[16];
   __shared__ int lds_set[16];
   double2 far = make_double2(0, 0);
   for (int64_t from = (a.tiles - 1) / 1024 * 1024; from >= 0; from -= 1024) {
@@ -460,7 +472,7 @@ __global__ __launch_bounds__(1024) void k_gae_tiles(GaeArgs a) {
 __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
   __shared__ GaeEnds ends;
   __shared__ Affine lds[2][4];
-  __shared__ double lds_v[2][4];
+  __shared__ float lds_v[2][4];
   __shared__ int lds_set[2][4];
   const int64_t tile = blockIdx.x;
   double2 in = make_double2(0, 0);
@@ -483,21 +495,20 @@ __global__ __launch_bounds__(256) void k_token_gae(GaeArgs a) {
   }
   GaeTile t;
   gae_load(a, tile, a.tiles > 1 ? a.map[tile].offset : -1, ends, t);
-  double v = 0;
+  float v;
   const bool set = gae_front(t, &v);
-  double V = block_value<4>(set, v, in.y, lds_v[0], lds_set[0], nullptr, nullptr);
-  double A = apply(block_behind<4>(gae_map(a, t, V), lds[0], nullptr), in.x);
+  const float V = block_value<4>(set, v, (float)in.y, lds_v[0], lds_set[0], nullptr, nullptr);
+  double delta[GAE_PER];
+  double A = apply(block_behind<4>(gae_map(a, t, V, delta), lds[0], nullptr), in.x);
   const double gl = a.gamma * a.lambda;
   float adv[GAE_PER], ret[GAE_PER];
 #pragma unroll
   for (int k = GAE_PER - 1; k >= 0; --k) {
     const bool on = t.on >> k & 1, end = t.end >> k & 1;
-    const double v = t.v[k];
-    if (end) { A = 0; V = t.last[k]; }
-    const double next = gl * A + (a.gamma * V + ((double)t.r[k] - v));
-    if (on) { A = next; V = v; }
+    if (end) A = 0;
+    if (on) A = gl * A + delta[k];
     adv[k] = on ? (float)A : 0.f;
-    ret[k] = on ? (float)(A + v) : 0.f;
+    ret[k] = on ? (float)(A + (double)t.v[k]) : 0.f;
   }
   const int64_t i = tile * GAE_TILE + threadIdx.x * GAE_PER;
   if (tile * GAE_TILE + GAE_TILE <= a.tokens) {

@@ -12,6 +12,7 @@ import ctypes as C
 import os
 
 import numpy as np
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libppo_learner.so")
@@ -121,8 +122,8 @@ def load_library():
 
 
 def load_binding(lib):
-    """The native module that makes the per-step calls, handed the library's functions."""
-    import torch  # noqa: F401  (its libraries must be loaded first)
+    """The native module that makes the per-step calls and those of the operators, handed the library's functions (torch, whose
+    libraries it needs, is imported above)."""
     try:
         from . import _binding
     except ImportError as e:
@@ -242,7 +243,6 @@ def permutation_static(S: int, seed: int, update_idx: int, epoch: int, out=None,
 # current stream of that device, and with another one the results belong to it (inputs must be ready on it, as with any stream).
 
 def _on_stream(first, stream, call, *args):
-    import torch
     if not isinstance(first, torch.Tensor) or not first.is_cuda:
         raise ValueError("expected a CUDA tensor")
     if stream is None:
