@@ -333,7 +333,7 @@ __device__ __forceinline__ void loss_idle(const RowArgs& a, int64_t row) {
 
 // Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers (as it is, 16 bits packed) between
 // the passes that find the maximum, add up and write, so that memory sees it once in and once out.  Exponentials are made twice; 18 to 22
-// vector instructions a logit of 16 bits keep the vector units busy for 0.63 of the time of its bytes (16384 x 131072).
+// vector instructions a logit of 16 bits keep the vector units busy for 0.6 of the time of its bytes (16384 x 131072).
 template <class T, int G, int K, bool ENT>
 __global__ __launch_bounds__(G < 256 ? 256 : G, K >= 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
   constexpr int NT = G < 256 ? 256 : G, N = Piece<T>::N;

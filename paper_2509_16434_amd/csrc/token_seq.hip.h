@@ -10,7 +10,7 @@ __device__ __forceinline__ int64_t hold(int64_t o, int64_t tokens) { return o < 
 // D = S_chosen - S_rejected; loss of a pair -(1 - ls) log sigmoid(bD) - ls log sigmoid(-bD), or (D - 1/(2b))^2.  D is a small
 // difference of long sums: they are held in 64 bits.  A pair with no unmasked token in one of its sequences adds nothing.
 // 13 bytes a token move; what a call costs is its two launches and the latency of the longest sequence's chain of loads
-// (2 M tokens in 512 sequences of uneven length: 7.8 us for the sums, 8.4 for the gradient; 4 us at the rate of a copy).
+// (2 M tokens in 512 sequences of uneven length: 7.6 us for the sums, 8.5 for the gradient; 4 and 2 at the rate of a copy).
 struct PairArgs {
   int64_t pairs, tokens;
   const float *logp, *ref;   // ref: may be NULL
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(1024) void k_pair_stats_join(int blocks, float scal
 // own by itself, and one tile needs nothing else.  A sum over a long sequence (gamma lambda = 1) is held in 64 bits.
 //
 // Bound: 16 to 17 bytes a token, the inputs twice (from the last-level cache the second time) where there is more than one tile:
-// 3 M tokens 10.0 + 15.0 us, 11 at the rate of a copy; 200000 tokens 5.3 + 6.3 us, which is latency.
+// 3 M tokens 9.8 + 14.6 us, 11 at the rate of a copy; 200000 tokens 5.2 + 6.4 us, which is latency.
 constexpr int GAE_PER = 8, GAE_TILE = 256 * GAE_PER;   // tokens per thread and per tile
 constexpr int GAE_DIRECT = 4096;                       // at most so many tiles are scanned directly
 struct GaeMap { double a, b, c; float v; int32_t set, stop, offset; };   // set: V -> v, else V stays; stop: nothing from behind
