@@ -292,7 +292,7 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
  * (exp x - x - 1: the non-negative one-sample estimate of KL(policy || reference)), and L = scale sum_r weight_r l_r over
  * the rows that are not idle.  At ties the unclipped branch carries the gradient. */
 typedef struct {
-  float temperature;      /* > 0 */
+  float temperature;      /* > 0, and large enough for 2 / temperature to be finite */
   float clip_lo, clip_hi; /* >= 0; clip_lo <= 1 */
   float kl_coef;          /* >= 0; without d_logp_ref it must be 0.  0 with one: the estimate is reported only */
   float ent_coef;         /* 0: the entropy is neither computed nor reported */

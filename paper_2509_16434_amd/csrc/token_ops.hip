@@ -38,6 +38,7 @@ constexpr int64_t MAX_COLS = (int64_t)1 << 30, MAX_STRIDE = (int64_t)1 << 40, MA
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 bool finite_in(double v, double lo, double hi) { return v >= lo && v <= hi; }
+bool usable_temperature(float t) { return t > 0 && isfinite(t) && isfinite(2.f / t); }  // log2(e) / t is a factor in the kernels
 bool aligned(const void* p, int bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 int elem_bytes(int32_t dtype) { return dtype == 0 ? 4 : 2; }
 
@@ -196,7 +197,7 @@ int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab) {
 int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target, float temperature, float* d_logp,
                    float* d_entropy, float* d_stat, void* d_ws, int64_t ws_bytes, void* hip_stream) {
   CHECK(check_sizes(dtype, rows, vocab));
-  if (!(temperature > 0) || !isfinite(temperature) || !isfinite(1.f / temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (!usable_temperature(temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0, and so must 2 / temperature");
   if (rows == 0) return PPO_OK;
   CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));
   CHECK(check_array("d_target", d_target, 4, true));
@@ -231,7 +232,7 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
                             const float* d_stat, const float* d_dlogp, const float* d_entropy, const float* d_dentropy, void* d_dlogits, int64_t ld_d,
                             void* hip_stream) {
   CHECK(check_sizes(dtype, rows, vocab));
-  if (!(temperature > 0) || !isfinite(temperature) || !isfinite(1.f / temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (!usable_temperature(temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0, and so must 2 / temperature");
   if (rows == 0) return PPO_OK;
   CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));
   CHECK(check_rows("d_dlogits", d_dlogits, dtype, vocab, ld_d));
@@ -267,7 +268,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
                    float* d_logp, float* d_stats, void* d_ws, int64_t ws_bytes, void* hip_stream) {
   CHECK(check_sizes(dtype, rows, vocab));
   if (!hp) return fail(PPO_EINVAL, "hp is NULL");
-  if (!(hp->temperature > 0) || !isfinite(hp->temperature) || !isfinite(1.f / hp->temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0");
+  if (!usable_temperature(hp->temperature)) return fail(PPO_EINVAL, "temperature must be finite and > 0, and so must 2 / temperature");
   if (!finite_in(hp->clip_lo, 0, 1) || !(hp->clip_hi >= 0) || !isfinite(hp->clip_hi)) return fail(PPO_EINVAL, "clip_lo must be in [0, 1] and clip_hi finite and >= 0");
   if (!(hp->kl_coef >= 0) || !isfinite(hp->kl_coef)) return fail(PPO_EINVAL, "kl_coef must be finite and >= 0");
   if (hp->kl_coef > 0 && rows > 0 && !d_logp_ref) return fail(PPO_EINVAL, "kl_coef > 0 needs d_logp_ref");
@@ -333,7 +334,7 @@ int ppo_pair_loss(int64_t pairs, int64_t tokens, const float* d_logp, const floa
   const int64_t items = 2 * pairs * g.slices;
   const uint32_t extra = a.record ? 0 : 1;   // the block of the statistics
   const int64_t mean = pairs > 0 ? tokens / (2 * pairs) : 0;
-  if (pairs > 0 && mean <= 64) {
+  if (pairs >= 2048 && mean <= 64) {
     hipLaunchKernelGGL(k_pair_sums<16>, dim3((uint32_t)cdiv(items, 16)), dim3(256), 0, st, a, g);
     hipLaunchKernelGGL(k_pair_loss<16>, dim3((uint32_t)cdiv(items, 16) + extra), dim3(256), 0, st, a, g);
   } else if (pairs >= 2048 && mean <= 512) {

@@ -35,7 +35,8 @@ __device__ __forceinline__ double pair_slope(int kind, double beta, double ls, d
 }
 
 // What a launch of the two kernels below knows of the grid: a sequence is worked on by `slices` groups of G threads, four tokens a
-// thread at a time; G = 16 or 64 threads for many short sequences (200000 of 10 tokens: 156 us by waves), blocks for long ones.
+// thread at a time; blocks of G = 256, and G = 16 or 64 threads where there are many short sequences (200000 of 10 tokens: 156 us by
+// waves, 48 by 16 threads; one that is long among them takes a thread's chain of loads of its length / 4 G).
 struct PairGrid {
   int32_t slices;
   double2* part;       // [2 * pairs][slices]: sum of an unmasked sequence's terms, and how many

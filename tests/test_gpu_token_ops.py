@@ -349,6 +349,10 @@ def test_no_rows():
     assert stats.tolist() == [0.0] * 7
     dlogp, margin, stats = L.pair_loss(torch.full((700,), 3.0, device="cuda"), off)   # tokens, but no pair
     assert dlogp.tolist() == [0.0] * 700 and stats.tolist() == [0.0] * 7
+    dlogp, margin, stats = L.pair_loss(z, torch.zeros(9, dtype=torch.int64, device="cuda"))   # pairs, but no token
+    assert dlogp.shape == (0,) and margin.tolist() == [0.0] * 4 and stats.tolist() == [0.0] * 7
+    for a in L.token_gae(torch.ones(5000, device="cuda"), torch.ones(5000, device="cuda"), off, 0.9, 0.9):   # tokens, but no sequence
+        assert not bool(a.any())
     # only idle rows
     x, t = torch.randn(3, 5, device="cuda"), torch.full((3,), -1, dtype=torch.int32, device="cuda")
     d, stats, logp = L.token_loss(x, t, x[:, 0].contiguous(), x[:, 1].contiguous(), ent_coef=0.5)
@@ -363,7 +367,7 @@ def cuts(lengths, before=0, behind=0):
 
 
 PAIR_LENGTHS = [([1], [1]), ([0], [5]), ([3, 0, 64, 1], [2, 0, 65, 1]), ([5000], [1]), ([257, 1000, 31], [513, 2, 4099]), ([1] * 300, [2] * 300), ([100003, 7], [50001, 9]),
-                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1))), ([5] * 256, [3] * 256), ([5] * 257, [3] * 257), ([700] * 130, [90] * 130), ([6000] * 20, [9000] * 20), ([2] * 5000, [1] * 5000)]
+                ([0, 0], [0, 0]), (list(range(40)), list(range(40, 0, -1))), ([5] * 256, [3] * 256), ([5] * 257, [3] * 257), ([700] * 130, [90] * 130), ([6000] * 20, [9000] * 20), ([2] * 5000, [1] * 5000), ([150] * 2100, [90] * 2100)]
 
 
 def pair_definition(logp, ref, keep, off, pairs, kind, beta, ls, mean, scale):
