@@ -246,7 +246,7 @@ int ppo_forward(ppo_ctx* ctx, const int32_t* d_idx, int64_t count, float* d_mu, 
  * They need no context and allocate nothing: every array is the caller's, results included.  Work is enqueued on
  * hip_stream (a hipStream_t, may be NULL) of the CURRENT device, where all arrays must lie; nothing synchronises, and
  * every call may be recorded into a graph.  d_ws is scratch of at least the bytes that the *_ws_bytes function gives
- * for the same sizes, 16-byte aligned; nothing is kept in it between calls, and two calls whose work may overlap in time
+ * for the same sizes (0: d_ws may be NULL), 16-byte aligned; nothing is kept in it between calls, and two calls whose work may overlap in time
  * need two of them (so do two captured graphs that may).  Errors are reported through ppo_last_error(NULL); arguments are
  * checked before any HIP call.  The same call gives the same results, bit for bit, every time (the order in which a row is added
  * up goes by its length, its alignment and the number of rows).  An empty call (no rows, tokens or
@@ -275,7 +275,7 @@ int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int6
  * d_target int32 [rows].  A row is IDLE if its target lies outside [0, vocab) - its logits are not read then - or if all of
  * its logits are -infinity: logp and H are 0.  A NaN or +infinity among the logits of any other row gives NaN.
  * d_entropy may be NULL.  d_stat (may be NULL): fp32 [rows][2], what the backward pass needs of the row. */
-int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab);
+int64_t ppo_token_logp_ws_bytes(int64_t rows, int64_t vocab);
 int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target,
                    float temperature, float* d_logp, float* d_entropy, float* d_stat, void* d_ws, int64_t ws_bytes, void* hip_stream);
 /* Gradient of sum_r (dlogp_r logp_r + dentropy_r H_r) by the logits, rounded once to their type:
@@ -302,6 +302,7 @@ typedef struct {
  * rows.  Outputs: d_dlogits (dL/dlogits; may be d_logits with the same row stride), d_logp [rows] (may be NULL), d_stats [8]:
  *   0 L, 1..3 its weighted sums scale sum w (-min(..)), scale sum w (exp x - x - 1), scale sum w H, then over the rows that are
  *   not idle 4 mean of (rho - 1) - log rho, 5 share with rho outside the clip range, 6 their number, 7 1 if L is not finite. */
+int64_t ppo_token_loss_ws_bytes(int64_t rows, int64_t vocab);
 int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_logits, int64_t ld, const int32_t* d_target,
                    const float* d_logp_old, const float* d_logp_ref, const float* d_adv, const float* d_weight,
                    const ppo_token_hparams* hp, void* d_dlogits, int64_t ld_d, float* d_logp, float* d_stats, void* d_ws,

@@ -17,9 +17,10 @@ decltype(&ppo_act) f_act = nullptr;
 decltype(&ppo_buffer_write_outcome) f_outcome = nullptr;
 decltype(&ppo_gae) f_gae = nullptr;
 decltype(&ppo_dropout) f_dropout = nullptr;
-decltype(&ppo_token_ws_bytes) f_token_ws = nullptr;
+decltype(&ppo_token_logp_ws_bytes) f_token_logp_ws = nullptr;
 decltype(&ppo_token_logp) f_token_logp = nullptr;
 decltype(&ppo_token_logp_backward) f_token_logp_backward = nullptr;
+decltype(&ppo_token_loss_ws_bytes) f_token_loss_ws = nullptr;
 decltype(&ppo_token_loss) f_token_loss = nullptr;
 decltype(&ppo_pair_ws_bytes) f_pair_ws = nullptr;
 decltype(&ppo_pair_loss) f_pair_loss = nullptr;
@@ -68,13 +69,13 @@ bool arity(Py_ssize_t got, Py_ssize_t want, const char* name) {
 // setup(addresses of ppo_buffer_write, ppo_buffer_write_range, ppo_act, ppo_buffer_write_outcome, ppo_gae, then of the operators
 // in the order of their declaration)
 PyObject* py_setup(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  long long v[14];
-  if (!arity(n, 14, "setup") || !integers(a, 14, v)) return nullptr;
-  f_dropout = reinterpret_cast<decltype(f_dropout)>(v[5]); f_token_ws = reinterpret_cast<decltype(f_token_ws)>(v[6]);
+  long long v[15];
+  if (!arity(n, 15, "setup") || !integers(a, 15, v)) return nullptr;
+  f_dropout = reinterpret_cast<decltype(f_dropout)>(v[5]); f_token_logp_ws = reinterpret_cast<decltype(f_token_logp_ws)>(v[6]);
   f_token_logp = reinterpret_cast<decltype(f_token_logp)>(v[7]); f_token_logp_backward = reinterpret_cast<decltype(f_token_logp_backward)>(v[8]);
-  f_token_loss = reinterpret_cast<decltype(f_token_loss)>(v[9]); f_pair_ws = reinterpret_cast<decltype(f_pair_ws)>(v[10]);
-  f_pair_loss = reinterpret_cast<decltype(f_pair_loss)>(v[11]); f_token_gae_ws = reinterpret_cast<decltype(f_token_gae_ws)>(v[12]);
-  f_token_gae = reinterpret_cast<decltype(f_token_gae)>(v[13]);
+  f_token_loss_ws = reinterpret_cast<decltype(f_token_loss_ws)>(v[9]); f_token_loss = reinterpret_cast<decltype(f_token_loss)>(v[10]);
+  f_pair_ws = reinterpret_cast<decltype(f_pair_ws)>(v[11]); f_pair_loss = reinterpret_cast<decltype(f_pair_loss)>(v[12]);
+  f_token_gae_ws = reinterpret_cast<decltype(f_token_gae_ws)>(v[13]); f_token_gae = reinterpret_cast<decltype(f_token_gae)>(v[14]);
   f_write = reinterpret_cast<decltype(f_write)>(v[0]); f_write_range = reinterpret_cast<decltype(f_write_range)>(v[1]);
   f_act = reinterpret_cast<decltype(f_act)>(v[2]); f_outcome = reinterpret_cast<decltype(f_outcome)>(v[3]); f_gae = reinterpret_cast<decltype(f_gae)>(v[4]);
   Py_RETURN_NONE;
@@ -308,7 +309,7 @@ PyObject* py_token_logp(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* st = stream_of(a[0]);
     const c10::DeviceGuard on(x.device());
     at::Tensor logp = floats(rows, x), entropy = ent ? floats(rows, x) : at::Tensor(), stat = at::empty({rows, 2}, logp.options());
-    const int64_t wsb = f_token_ws(rows, V);
+    const int64_t wsb = f_token_logp_ws(rows, V);
     const at::Tensor ws = scratch(wsb, x);
     const int rc = without_lock([&] {
       return f_token_logp(dt, rows, V, x.data_ptr(), ld, ptr<const int32_t>(target), (float)temperature, ptr<float>(logp), ptr<float>(entropy), ptr<float>(stat), ptr<void>(ws), wsb, st);
@@ -360,7 +361,7 @@ PyObject* py_token_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int64_t ldd = row_stride(d, "out");
     apart_or_same(d, ldd, x, ld, "logits");
     at::Tensor logp = floats(rows, x), stats = floats(8, x);
-    const int64_t wsb = f_token_ws(rows, V);
+    const int64_t wsb = f_token_loss_ws(rows, V);
     const at::Tensor ws = scratch(wsb, x);
     const int rc = without_lock([&] {
       return f_token_loss(dt, rows, V, x.data_ptr(), ld, ptr<const int32_t>(target), ptr<const float>(old), ptr<const float>(ref), ptr<const float>(adv), ptr<const float>(weight),

@@ -1,6 +1,8 @@
 // Element types of the operators that take fp32, bf16 or fp16 arrays, to and from fp32, and the 16-byte pieces that they are
 // read and written in.
 #pragma once
+#include <utility>
+
 #include "common.hip.h"
 
 typedef _Float16 f16_t;
@@ -16,6 +18,15 @@ typedef u32x4_t u32x4_any_t __attribute__((aligned(2)));
 // From here on the compiler knows nothing of a piece's value, so that it unpacks it again in the next pass over the row instead of
 // keeping all of it in 32 bits (which needs two to four times the registers).
 __device__ __forceinline__ void forget(u32x4_t& v) { asm volatile("" : "+v"(v)); }
+// K pieces in registers, each a variable of its own, and f(0), ..., f(K - 1) with the number as a constant to go over them.  (An array of 4
+// or 8 pieces is taken for one vector of 16 or 32 registers in a row, which every condition on the way copies as a whole: 304 registers,
+// or thousands of spills.)
+#define INLINE __attribute__((always_inline))
+template <int K> struct Pieces : Pieces<K - 1> { u32x4_t v; };
+template <> struct Pieces<0> {};
+template <int k, int K> __device__ __forceinline__ u32x4_t& piece(Pieces<K>& p) { return static_cast<Pieces<k + 1>&>(p).v; }
+template <class F, int... k> __device__ __forceinline__ void each_of(std::integer_sequence<int, k...>, F f) { (f(std::integral_constant<int, k>()), ...); }
+template <int K, class F> __device__ __forceinline__ void each(F f) { each_of(std::make_integer_sequence<int, K>(), f); }
 template <class T> struct Piece { static constexpr int N = 16 / sizeof(T); };
 template <class T> __device__ __forceinline__ u32x4_t load_piece(const T* p) { return *reinterpret_cast<const u32x4_any_t*>(p); }
 template <class T> __device__ __forceinline__ void store_piece(T* p, u32x4_t v) { *reinterpret_cast<u32x4_any_t*>(p) = v; }

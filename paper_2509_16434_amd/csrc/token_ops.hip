@@ -89,11 +89,16 @@ void set_slices(RowArgs& a, int64_t most_rows) {
   a.slices = (int32_t)cdiv(a.vocab, a.slice_len);
 }
 
-// Workspace of a call on rows: parts of the slices (16 bytes each), records of the loss, then sums of the blocks that add those up.
+// Workspace of a call on rows: parts of the slices (16 bytes each); for the loss then the rows' records and the sums of the blocks that
+// add those up, or nothing where one block does it all.
+int64_t parts_bytes(int64_t rows, int64_t vocab, int64_t most_rows) {
+  const int s = slices_of(std::max<int64_t>(rows, 1), vocab, most_rows);
+  return s > 1 ? rows * s * 16 : 0;
+}
+bool small_loss(int64_t rows, int64_t vocab) { return rows <= SMALL_ROWS && vocab <= SMALL_VOCAB; }
 int stats_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, STATS_ROWS), 1024)); }
 int64_t stats_offset(int64_t rows, int64_t vocab) {
-  const int s = slices_of(std::max<int64_t>(rows, 1), vocab, SLICED_ROWS);
-  return ((s > 1 ? rows * s * 16 : 0) + rows * (int64_t)sizeof(LossRecord) + 15) / 16 * 16;
+  return (parts_bytes(rows, vocab, SLICED_LOSS_ROWS) + rows * (int64_t)sizeof(LossRecord) + 15) / 16 * 16;
 }
 
 // f(element type) for the type named by dtype
@@ -120,7 +125,7 @@ void with_flag(bool on, F f) {
 }
 
 // The kernel of a loss: the narrowest group whose registers hold the row; four rows a wave (16 threads each) are 131072 rows of 257 in
-// 48 us where one is 86, but fewer and longer chains for few rows (448 of 256: 4.9 and 3.4 us).
+// 39 us where one is 86, but fewer and longer chains for few rows (448 of 256: 4.9 and 3.4 us).
 template <class T, bool ENT>
 void launch_loss(const RowArgs& a, hipStream_t st) {
   const int64_t pieces = cdiv(a.vocab, Piece<T>::N);
@@ -189,8 +194,14 @@ int ppo_dropout(int32_t dtype, int64_t rows, int64_t cols, const void* d_x, int6
   return PPO_OK;
 }
 
-int64_t ppo_token_ws_bytes(int64_t rows, int64_t vocab) {
+int64_t ppo_token_logp_ws_bytes(int64_t rows, int64_t vocab) {
   if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return PPO_ESHAPE;
+  return parts_bytes(rows, vocab, SLICED_ROWS);
+}
+
+int64_t ppo_token_loss_ws_bytes(int64_t rows, int64_t vocab) {
+  if (rows < 0 || rows > MAX_ROWS || vocab < 1 || vocab > PPO_TOKEN_MAX_VOCAB) return PPO_ESHAPE;
+  if (small_loss(rows, vocab)) return 0;
   return stats_offset(rows, vocab) + (stats_blocks(rows) > 1 ? stats_blocks(rows) * 48 : 0);
 }
 
@@ -204,7 +215,7 @@ int ppo_token_logp(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   CHECK(check_array("d_logp", d_logp, 4, true));
   CHECK(check_array("d_entropy", d_entropy, 4, false));
   CHECK(check_array("d_stat", d_stat, 4, false));
-  CHECK(check_ws(d_ws, ws_bytes, ppo_token_ws_bytes(rows, vocab)));
+  CHECK(check_ws(d_ws, ws_bytes, ppo_token_logp_ws_bytes(rows, vocab)));
   RowArgs a = {};
   a.rows = rows; a.ld = ld; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / temperature;
   a.logp = d_logp; a.entropy = d_entropy; a.stat = d_stat;
@@ -283,13 +294,25 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
     CHECK(check_array("d_adv", d_adv, 4, true));
     CHECK(check_array("d_weight", d_weight, 4, false));
     CHECK(check_array("d_logp", d_logp, 4, false));
-    CHECK(check_ws(d_ws, ws_bytes, ppo_token_ws_bytes(rows, vocab)));
+    CHECK(check_ws(d_ws, ws_bytes, ppo_token_loss_ws_bytes(rows, vocab)));
   }
   RowArgs a = {};
   a.rows = rows; a.ld = ld; a.ldd = ld_d; a.vocab = (int32_t)vocab; a.logits = d_logits; a.target = d_target; a.inv_t = 1.f / hp->temperature;
   a.logp = d_logp; a.dlogits = d_dlogits; a.logp_old = d_logp_old; a.logp_ref = d_logp_ref; a.adv = d_adv; a.weight = d_weight;
   a.clip_lo = hp->clip_lo; a.clip_hi = hp->clip_hi; a.kl_coef = hp->kl_coef; a.ent_coef = hp->ent_coef; a.scale = hp->scale;
   hipStream_t st = (hipStream_t)hip_stream;
+  if (small_loss(rows, vocab)) {
+    with_type(dtype, [&](auto t) {
+      with_flag(hp->ent_coef != 0.f, [&](auto ent) {
+        using T = decltype(t);
+        constexpr bool ENT = decltype(ent)::value;
+        if (vocab <= 16 * 4 * Piece<T>::N) hipLaunchKernelGGL((k_token_loss_small<T, 4, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
+        else hipLaunchKernelGGL((k_token_loss_small<T, 8, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
+      });
+    });
+    LAUNCHCHK("k_token_loss_small");
+    return PPO_OK;
+  }
   if (rows > 0) {
     set_slices(a, SLICED_LOSS_ROWS);
     a.part = (float*)d_ws;

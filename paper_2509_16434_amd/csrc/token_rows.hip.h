@@ -14,7 +14,7 @@
 //
 // Measured (GB/s of one read and, for gradients, one write of every logit; a plain copy of 2 GiB reaches 4490, reading alone 5200):
 //   log-probability   8192 x 50257 fp16 5790, 8192 x 131072 bf16 6040, 65536 x 1000 bf16 5100
-//   loss              16384 x 131072 bf16 5480, 8192 x 32000 bf16 5090, 3001 x 50257 bf16 with entropy 4920, 131072 x 257 bf16 2870
+//   loss              16384 x 131072 bf16 5480, 8192 x 32000 bf16 5090, 3001 x 50257 bf16 with entropy 4900, 32768 x 2000 bf16 4950, 131072 x 257 bf16 3560
 //   backward          4096 x 32000 fp32 5800
 #pragma once
 #include "elem.hip.h"
@@ -123,19 +123,13 @@ __device__ __forceinline__ RowStat stream_stat(const T* x, int n, int tid, float
   else if (r.mx != r.mx) r = RowStat{-INFINITY, NAN, NAN};
   x += q.head;
   for (int i = tid * N; i < q.full; i += G * N * U) {
-    u32x4_t v[U];
+    Pieces<U> v;
     float m = r.mx;
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G * N < q.full) v[u] = load_piece(x + i + u * G * N);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G * N < q.full) m = fmaxf(m, max_piece<T>(v[u]));
+    each<U>([&](auto u) INLINE { if (i + u * G * N < q.full) piece<u>(v) = load_piece(x + i + u * G * N); });
+    each<U>([&](auto u) INLINE { if (i + u * G * N < q.full) m = fmaxf(m, max_piece<T>(piece<u>(v))); });
     r = rebase<ENT>(r, m, c);
     const float base = r.base();
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G * N < q.full) add_piece<T, ENT>(r, v[u], base, c);
+    each<U>([&](auto u) INLINE { if (i + u * G * N < q.full) add_piece<T, ENT>(r, piece<u>(v), base, c); });
   }
   return r;
 }
@@ -275,13 +269,9 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
   const int slice = G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N), r = t - q.head;
   const bool owner = r >= 0 && r < q.full ? r >= slice && r < slice + G * BACK_PIECES * N && (r - slice) / N % G == tid : t == q.one;
   const float xt = owner ? to_f(x[t]) : 0.f, xl = q.one >= 0 ? to_f(x[q.one]) : 0.f;
-  u32x4_t v[BACK_PIECES];
-#pragma unroll
-  for (int u = 0; u < BACK_PIECES; ++u)
-    if (from + u * G * N < q.full) v[u] = load_piece(x + q.head + from + u * G * N);
-#pragma unroll
-  for (int u = 0; u < BACK_PIECES; ++u)
-    if (from + u * G * N < q.full) store(y + q.head + from + u * G * N, grad_piece<T, ENT>(v[u], k));
+  Pieces<BACK_PIECES> v;
+  each<BACK_PIECES>([&](auto u) INLINE { if (from + u * G * N < q.full) piece<u>(v) = load_piece(x + q.head + from + u * G * N); });
+  each<BACK_PIECES>([&](auto u) INLINE { if (from + u * G * N < q.full) store(y + q.head + from + u * G * N, grad_piece<T, ENT>(piece<u>(v), k)); });
   if (q.one >= 0) y[q.one] = from_f<T>(grad_one<ENT>(xl, k));
   if (owner) y[t] = from_f<T>(grad_one<ENT>(xt, k) + k.add);
 }
@@ -317,71 +307,63 @@ __device__ __forceinline__ LossTerm loss_term(const RowArgs& a, const LossIn& in
   o.g *= in.w; o.h *= in.w;
   return o;
 }
-__device__ __forceinline__ GradCoef loss_row(const RowArgs& a, int64_t row, const LossIn& in, const RowStat& r, float xt, bool ent, bool writes) {
+// The record of a row and the coefficients of its gradient; one thread (writes) leaves the log-probability.
+__device__ __forceinline__ GradCoef loss_row(const RowArgs& a, int64_t row, const LossIn& in, const RowStat& r, float xt, bool ent, bool writes, LossRecord* rec) {
   const RowOut o = row_out(r, xt, a.inv_t, ent);
   const LossTerm l = loss_term(a, in, o.logp, o.ent);
-  if (writes) {
-    if (a.logp) a.logp[row] = o.logp;
-    ((LossRecord*)a.record)[row] = l.rec;
-  }
+  if (writes && a.logp) a.logp[row] = o.logp;
+  *rec = l.rec;
   return grad_coef(l.g, l.h, o.ent, o.ls, r.base(), a.inv_t / r.s, a.inv_t);
 }
-__device__ __forceinline__ void loss_idle(const RowArgs& a, int64_t row) {
-  if (a.logp) a.logp[row] = 0.f;
-  ((LossRecord*)a.record)[row] = LossRecord{0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+template <class T>
+__device__ __forceinline__ LossRecord loss_idle(const RowArgs& a, int64_t row, T* y, int n, int tid, int G, bool writes) {
+  zero_row(y, n, tid, G);
+  if (writes && a.logp) a.logp[row] = 0.f;
+  return LossRecord{0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 }
 
 // Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers (as it is, 16 bits packed) between
 // the passes that find the maximum, add up and write, so that memory sees it once in and once out.  Exponentials are made twice; 18 to 22
 // vector instructions a logit of 16 bits keep the vector units busy for 0.6 of the time of its bytes (16384 x 131072).
 template <class T, int G, int K, bool ENT>
-__global__ __launch_bounds__(G < 256 ? 256 : G, K >= 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
-  constexpr int NT = G < 256 ? 256 : G, N = Piece<T>::N;
-  __shared__ float lds[3 * (NT / 64)];
-  const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);
-  if (G < 256 && row >= a.rows) return;   // G <= 64: no barrier follows
-  const int t = a.target[row], tid = threadIdx.x % G, at = tid * N;
+__device__ __forceinline__ LossRecord loss_in_registers(const RowArgs& a, int64_t row, int tid, float* lds) {
+  constexpr int N = Piece<T>::N;
+  const int t = a.target[row], at = tid * N;
   const T* x = (const T*)a.logits + row * a.ld;
   T* y = (T*)a.dlogits + row * a.ldd;
-  if (t < 0 || t >= a.vocab) {
-    zero_row(y, a.vocab, tid, G);
-    if (tid == 0) loss_idle(a, row);
-    return;
-  }
+  if (t < 0 || t >= a.vocab) return loss_idle(a, row, y, a.vocab, tid, G, tid == 0);
   const float c = a.inv_t * TOKEN_LOG2E;
   const LossIn in = loss_in(a, row);
   float xt = to_f(x[t]);
   const Cut w = cut_row(x, a.vocab, tid);
-  const int full = w.full;
   const float xl = w.one >= 0 ? to_f(x[w.one]) : -INFINITY;
-  u32x4_t v[K];
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (at + k * G * N < full) v[k] = load_piece(x + w.head + at + k * G * N);
+  Pieces<K> v;
+  each<K>([&](auto k) INLINE { if (at + k * G * N < w.full) piece<k>(v) = load_piece(x + w.head + at + k * G * N); });
   asm volatile("" : "+v"(xt));   // read before the barrier: the gradient may lie in the logits' memory
   float m = xl;
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (at + k * G * N < full) { m = fmaxf(m, max_piece<T>(v[k])); forget(v[k]); }
+  each<K>([&](auto k) INLINE { if (at + k * G * N < w.full) { m = fmaxf(m, max_piece<T>(piece<k>(v))); forget(piece<k>(v)); } });
   RowStat r = {lanes_max<G < 64 ? G : 64>(m), 0.f, 0.f};
   const float base = r.base();
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (at + k * G * N < full) { add_piece<T, ENT>(r, v[k], base, c); forget(v[k]); }
+  each<K>([&](auto k) INLINE { if (at + k * G * N < w.full) { add_piece<T, ENT>(r, piece<k>(v), base, c); forget(piece<k>(v)); } });
   if (w.one >= 0) add_one<ENT>(r, xl, base, c);
   r = group_join<G, ENT>(r, c, lds);
-  if (r.idle()) {
-    zero_row(y, a.vocab, tid, G);
-    if (tid == 0) loss_idle(a, row);
-    return;
-  }
-  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
-#pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (at + k * G * N < full) store_piece(y + w.head + at + k * G * N, grad_piece<T, ENT>(v[k], q));
+  if (r.idle()) return loss_idle(a, row, y, a.vocab, tid, G, tid == 0);
+  LossRecord rec;
+  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0, &rec);
+  each<K>([&](auto k) INLINE { if (at + k * G * N < w.full) store_piece(y + w.head + at + k * G * N, grad_piece<T, ENT>(piece<k>(v), q)); });
   if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
   // the target's element again, by the thread that wrote it with its piece
   if (owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
+  return rec;
+}
+template <class T, int G, int K, bool ENT>
+__global__ __launch_bounds__(G < 256 ? 256 : G, K >= 16 ? 4 : K == 8 ? 6 : K == 4 ? 4 : 8) void k_token_loss(RowArgs a) {
+  constexpr int NT = G < 256 ? 256 : G;
+  __shared__ float lds[3 * (NT / 64)];
+  const int64_t row = (int64_t)blockIdx.x * (NT / G) + (G < 256 ? threadIdx.x / G : 0);
+  if (G < 256 && row >= a.rows) return;   // G <= 64: no barrier follows
+  const LossRecord rec = loss_in_registers<T, G, K, ENT>(a, row, threadIdx.x % G, lds);
+  if (threadIdx.x % G == 0) ((LossRecord*)a.record)[row] = rec;
 }
 
 // The gradient of n elements by G threads; t: the target's place among them, if it is one of them.
@@ -391,13 +373,9 @@ __device__ __forceinline__ void stream_gradient(const T* x, T* y, int n, int tid
   const Cut w = cut_row(x, n, tid);
   const float xl = w.one >= 0 ? to_f(x[w.one]) : 0.f;
   for (int i = tid * N; i < w.full; i += G * N * U) {
-    u32x4_t v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G * N < w.full) v[u] = load_piece(x + w.head + i + u * G * N);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u * G * N < w.full) store_piece(y + w.head + i + u * G * N, grad_piece<T, ENT>(v[u], q));
+    Pieces<U> v;
+    each<U>([&](auto u) INLINE { if (i + u * G * N < w.full) piece<u>(v) = load_piece(x + w.head + i + u * G * N); });
+    each<U>([&](auto u) INLINE { if (i + u * G * N < w.full) store_piece(y + w.head + i + u * G * N, grad_piece<T, ENT>(piece<u>(v), q)); });
   }
   if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
   if (t >= 0 && t < n && owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
@@ -422,13 +400,13 @@ __global__ __launch_bounds__(1024) void k_token_loss_long(RowArgs a) {
     asm volatile("" : "+v"(xt));
     r = group_join<G, ENT>(stream_stat<T, G, ENT>(x, a.vocab, tid, c), c, lds);
   }
-  if (r.idle()) {
-    zero_row(y, a.vocab, tid, G);
-    if (tid == 0) loss_idle(a, row);
-    return;
+  LossRecord rec;
+  if (r.idle()) rec = loss_idle(a, row, y, a.vocab, tid, G, tid == 0);
+  else {
+    const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0, &rec);
+    stream_gradient<T, G, ENT>(x, y, a.vocab, tid, q, t, xt);
   }
-  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0);
-  stream_gradient<T, G, ENT>(x, y, a.vocab, tid, q, t, xt);
+  if (tid == 0) ((LossRecord*)a.record)[row] = rec;
 }
 
 // Few long rows: k_token_part has left the statistics of the slices; every slice's block joins them all and writes its gradient.
@@ -441,14 +419,14 @@ __global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
   const bool first = blockIdx.x == 0 && tid == 0;
   RowStat r = {-INFINITY, 0.f, 0.f};
   if (t >= 0 && t < a.vocab) r = join_parts<ENT>(a, row, a.inv_t * TOKEN_LOG2E);
-  if (r.idle()) {
-    zero_row(y, n, tid, 256);
-    if (first) loss_idle(a, row);
-    return;
+  LossRecord rec;
+  if (r.idle()) rec = loss_idle(a, row, y, n, tid, 256, first);
+  else {
+    const float xt = a.part[4 * row * a.slices + 3];
+    const GradCoef q = loss_row(a, row, loss_in(a, row), r, xt, ENT, first, &rec);
+    stream_gradient<T, 256, ENT>(x, y, n, tid, q, t - from, xt);
   }
-  const float xt = a.part[4 * row * a.slices + 3];
-  const GradCoef q = loss_row(a, row, loss_in(a, row), r, xt, ENT, first);
-  stream_gradient<T, 256, ENT>(x, y, n, tid, q, t - from, xt);
+  if (first) ((LossRecord*)a.record)[row] = rec;
 }
 
 // Statistics of the loss: the rows' records added in a fixed order, in 64 bits; `share` rows a block.  One block finishes
@@ -484,4 +462,19 @@ __global__ __launch_bounds__(1024) void k_token_stats_join(int blocks, float kl_
   for (int k = 0; k < 6; ++k) v[k] = (int)threadIdx.x < blocks ? part[6 * threadIdx.x + k] : 0.0;
   block_sums<16>(v, lds);
   if (threadIdx.x == 0) write_stats(v, kl_coef, ent_coef, stats);
+}
+
+// A few short rows by one block, statistics included (64 rows a turn): one launch and no workspace where these are what a call costs
+// (4 rows of 64: 10.3 -> 6.5 us a call).
+constexpr int SMALL_ROWS = 128, SMALL_VOCAB = 512;
+template <class T, int K, bool ENT>
+__global__ __launch_bounds__(1024) void k_token_loss_small(RowArgs a, float* stats) {
+  __shared__ double lds[6 * 16];
+  double v[6] = {0, 0, 0, 0, 0, 0};
+  for (int64_t row = threadIdx.x / 16; row < a.rows; row += 64) {
+    const LossRecord r = loss_in_registers<T, 16, K, ENT>(a, row, threadIdx.x % 16, nullptr);
+    if (threadIdx.x % 16 == 0) { v[0] += r.pi; v[1] += r.kl; v[2] += r.ent; v[3] += r.old_kl; v[4] += r.clipped; v[5] += r.active; }
+  }
+  block_sums<16>(v, lds);
+  if (threadIdx.x == 0) write_stats(v, a.kl_coef, a.ent_coef, stats);
 }

@@ -64,8 +64,8 @@ class LearnerError(RuntimeError):
         self.code = code
 
 
-OPERATORS = ("ppo_dropout", "ppo_token_ws_bytes", "ppo_token_logp", "ppo_token_logp_backward", "ppo_token_loss", "ppo_pair_ws_bytes",
-             "ppo_pair_loss", "ppo_token_gae_ws_bytes", "ppo_token_gae")
+OPERATORS = ("ppo_dropout", "ppo_token_logp_ws_bytes", "ppo_token_logp", "ppo_token_logp_backward", "ppo_token_loss_ws_bytes", "ppo_token_loss",
+             "ppo_pair_ws_bytes", "ppo_pair_loss", "ppo_token_gae_ws_bytes", "ppo_token_gae")
 
 
 def load_library():
@@ -102,7 +102,8 @@ def load_library():
         "distill_update": (C.c_int, [vp, C.POINTER(HParams), C.POINTER(MbStats)]),
         "ppo_forward": (C.c_int, [vp, vp, i64, vp, vp]),
         "ppo_dropout": (C.c_int, [i32, i64, i64, vp, i64, vp, vp, i64, C.c_double, u64, u64, vp, i64, vp]),
-        "ppo_token_ws_bytes": (i64, [i64, i64]),
+        "ppo_token_logp_ws_bytes": (i64, [i64, i64]),
+        "ppo_token_loss_ws_bytes": (i64, [i64, i64]),
         "ppo_token_logp": (C.c_int, [i32, i64, i64, vp, i64, vp, C.c_float, vp, vp, vp, vp, i64, vp]),
         "ppo_token_logp_backward": (C.c_int, [i32, i64, i64, vp, i64, vp, C.c_float, vp, vp, vp, vp, vp, i64, vp]),
         "ppo_token_loss": (C.c_int, [i32, i64, i64, vp, i64, vp, vp, vp, vp, vp, C.POINTER(TokenHParams), vp, i64, vp, vp, vp, i64, vp]),

@@ -58,8 +58,9 @@ def test_kernels_keep_their_rows_in_registers():
 
 def test_workspace_sizes():
     for rows, vocab in ((0, 1), (1, 1), (16, 131072), (1 << 20, 256), ((1 << 24) - 1, 2)):
-        assert 0 <= lib.ppo_token_ws_bytes(rows, vocab) <= 4096 * rows + (1 << 20)
-    assert lib.ppo_token_ws_bytes(-1, 8) == lib.ppo_token_ws_bytes(8, 0) == lib.ppo_token_ws_bytes(8, (1 << 24) + 1) == L.PPO_ESHAPE
+        for size in (lib.ppo_token_logp_ws_bytes, lib.ppo_token_loss_ws_bytes):
+            assert 0 <= size(rows, vocab) <= 4096 * rows + (1 << 20)
+            assert size(-1, 8) == size(8, 0) == size(8, (1 << 24) + 1) == L.PPO_ESHAPE
     assert lib.ppo_pair_ws_bytes(4, 100) >= 0 and lib.ppo_pair_ws_bytes(-1, 100) == lib.ppo_pair_ws_bytes(1, -1) == L.PPO_ESHAPE
     assert lib.ppo_token_gae_ws_bytes(4, 100) >= 0 and lib.ppo_token_gae_ws_bytes(1, -1) == lib.ppo_token_gae_ws_bytes(-1, 1) == L.PPO_ESHAPE
 
@@ -105,7 +106,7 @@ def test_token_logp_backward_refuses(change, code):
     assert lib.ppo_token_logp_backward(*dict(BACK, **change).values()) == code
 
 
-LOSS = dict(dtype=1, rows=4, vocab=8, x=P, ld=8, target=P, old=P, ref=NUL, adv=P, weight=NUL, hp=None, d=P, ldd=8, logp=P, stats=P, ws=P, wsb=1 << 20, st=NUL)
+LOSS = dict(dtype=1, rows=4, vocab=600, x=P, ld=600, target=P, old=P, ref=NUL, adv=P, weight=NUL, hp=None, d=P, ldd=600, logp=P, stats=P, ws=P, wsb=1 << 20, st=NUL)
 HP = dict(temperature=1.0, clip_lo=0.2, clip_hi=0.2, kl_coef=0.0, ent_coef=0.0, scale=1.0)
 
 
@@ -114,7 +115,7 @@ HP = dict(temperature=1.0, clip_lo=0.2, clip_hi=0.2, kl_coef=0.0, ent_coef=0.0, 
     ({}, dict(temperature=0.0), L.PPO_EINVAL), ({}, dict(clip_lo=1.5), L.PPO_EINVAL), ({}, dict(clip_lo=-0.1), L.PPO_EINVAL), ({}, dict(clip_hi=-1.0), L.PPO_EINVAL),
     ({}, dict(clip_hi=INF), L.PPO_EINVAL), ({}, dict(kl_coef=-0.1), L.PPO_EINVAL), ({}, dict(kl_coef=0.1), L.PPO_EINVAL),   # the last: no reference
     ({}, dict(ent_coef=NAN), L.PPO_EINVAL), ({}, dict(scale=INF), L.PPO_EINVAL), (dict(old=NUL), {}, L.PPO_EINVAL), (dict(adv=NUL), {}, L.PPO_EINVAL),
-    (dict(stats=NUL), {}, L.PPO_EINVAL), (dict(d=NUL), {}, L.PPO_EINVAL), (dict(ldd=7), {}, L.PPO_ESHAPE), (dict(ws=NUL), {}, L.PPO_EINVAL), (dict(wsb=8), {}, L.PPO_EINVAL),
+    (dict(stats=NUL), {}, L.PPO_EINVAL), (dict(d=NUL), {}, L.PPO_EINVAL), (dict(ldd=599), {}, L.PPO_ESHAPE), (dict(ws=NUL), {}, L.PPO_EINVAL), (dict(wsb=8), {}, L.PPO_EINVAL),
     (dict(ws=P + 8), {}, L.PPO_EINVAL), (dict(weight=P + 1), {}, L.PPO_EINVAL),
 ])
 def test_token_loss_refuses(change, hp, code):
