@@ -621,7 +621,7 @@ def everything_inputs(seed, rows, vocab):
     return x, target, old, ref, adv, off, mask, torch.randn(rows, 500, generator=g, device="cuda"), torch.randperm(rows, generator=g, device="cuda")
 
 
-@pytest.mark.parametrize("rows,vocab", [(40, 1000), (6, 40000), (600, 9000)])
+@pytest.mark.parametrize("rows,vocab", [(30, 200), (40, 1000), (6, 50000), (600, 9000)])
 def test_on_a_side_stream_and_in_graphs(rows, vocab):
     args = everything_inputs(1, rows, vocab)
     want = everything(*args)
