@@ -295,7 +295,7 @@ typedef struct {
   float temperature;      /* > 0, and large enough for 2 / temperature to be finite */
   float clip_lo, clip_hi; /* >= 0; clip_lo <= 1 */
   float kl_coef;          /* >= 0; without d_logp_ref it must be 0.  0 with one: the estimate is reported only */
-  float ent_coef;         /* 0: the entropy is neither computed nor reported */
+  float ent_coef;         /* 0: the entropy is neither computed nor reported; ent_coef * scale must be finite */
   float scale;            /* e.g. 1 / number of tokens; a loss scale for fp16 gradients */
 } ppo_token_hparams;
 /* Inputs [rows]: d_target, d_logp_old, d_adv; d_logp_ref, d_weight may be NULL (no KL; weights 1).  They are not read in idle

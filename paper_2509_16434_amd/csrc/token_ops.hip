@@ -283,7 +283,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
   if (!finite_in(hp->clip_lo, 0, 1) || !(hp->clip_hi >= 0) || !isfinite(hp->clip_hi)) return fail(PPO_EINVAL, "clip_lo must be in [0, 1] and clip_hi finite and >= 0");
   if (!(hp->kl_coef >= 0) || !isfinite(hp->kl_coef)) return fail(PPO_EINVAL, "kl_coef must be finite and >= 0");
   if (hp->kl_coef > 0 && rows > 0 && !d_logp_ref) return fail(PPO_EINVAL, "kl_coef > 0 needs d_logp_ref");
-  if (!isfinite(hp->ent_coef) || !isfinite(hp->scale)) return fail(PPO_EINVAL, "ent_coef and scale must be finite");
+  if (!isfinite(hp->ent_coef) || !isfinite(hp->scale) || !isfinite(hp->ent_coef * hp->scale)) return fail(PPO_EINVAL, "ent_coef, scale and their product must be finite");
   CHECK(check_array("d_stats", d_stats, 4, true));
   if (rows > 0) {
     CHECK(check_rows("d_logits", d_logits, dtype, vocab, ld));

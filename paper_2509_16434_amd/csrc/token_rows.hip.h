@@ -4,7 +4,8 @@
 //   z = x / temperature, m = max z, s = sum exp(z - m), p = exp(z - m) / s
 //   logp = z_t - m - log s,   H = log s - sum p (z - m)
 //   d/dx of g logp + h H:   [ g ([j = t] - p_j) - h p_j (log p_j + H) ] / temperature
-// The kernels work with d = x - max x (exact to one fp32 rounding whatever the size of x) and e = exp2(d c), c = log2(e) / temperature.
+// The kernels work with d = x - max x (exact to one fp32 rounding whatever the size of x), y = d c, c = log2(e) / temperature, and e = exp2(y).
+// Only y and e go into sums and gradients: d of a banned logit and powers of 1 / temperature may lie beyond fp32 where the result does not.
 // A row is idle when its target is outside [0, vocab) (its logits are not read then) or none of its logits is above -infinity:
 // log-probability, entropy and terms of the loss 0, gradient row 0.
 //
@@ -40,25 +41,26 @@ struct RowArgs {
 // What a row adds to the statistics of the loss.
 struct LossRecord { float pi, kl, ent, old_kl, clipped, active; };
 
-// max x, sum e, sum e d (with respect to the max; to 0 where it is -infinity).  idle(): nothing above -infinity, and no NaN.
+// max x, sum e, sum e y (with respect to the max; to 0 where it is -infinity).  idle(): nothing above -infinity, and no NaN.
 struct RowStat {
-  float mx, s, sd;
+  float mx, s, sy;
   __device__ __forceinline__ float base() const { return mx == -INFINITY ? 0.f : mx; }
   __device__ __forceinline__ bool idle() const { return mx == -INFINITY && s == 0.f; }
 };
 
 #define TOKEN_LOG2E 1.44269504088896340736f
+#define TOKEN_LN2 0.69314718055994530942f
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }  // 1 ulp; results below 2^-126 are 0
-// d of a logit of -infinity is -infinity: as a factor it is held at a finite value, so that 0 * d stays 0
-__device__ __forceinline__ float finite_d(float d) { return fmaxf(d, -1e30f); }
+// y of a logit of -infinity is -infinity: as a factor it is held where exp2 is 0 already, so that e y is 0
+__device__ __forceinline__ float finite_y(float y) { return fmaxf(y, -200.f); }
 
 // ---- statistics of parts of a row, joined
 // b's sums with respect to the maximum mx (>= b.mx)
 template <bool ENT>
 __device__ __forceinline__ RowStat rebase(RowStat b, float mx, float c) {
   const bool none = b.mx == -INFINITY;   // sums 0 (or NaN): no factor
-  const float d = none ? 0.f : b.mx - mx, f = exp2_hw(d * c);
-  if (ENT) b.sd = f * (b.sd + b.s * finite_d(d));
+  const float y = none ? 0.f : (b.mx - mx) * c, f = exp2_hw(y);
+  if (ENT) b.sy = f * (b.sy + b.s * finite_y(y));
   b.s *= f;
   b.mx = mx;
   return b;
@@ -70,12 +72,12 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
   constexpr int W = G < 64 ? G : 64;
   RowStat w = rebase<ENT>(r, lanes_max<W>(r.mx), c);
   w.s = lanes_sum<W>(w.s);
-  if (ENT) w.sd = lanes_sum<W>(w.sd);
+  if (ENT) w.sy = lanes_sum<W>(w.sy);
   if constexpr (G <= 64) return w;
   else {
     constexpr int NW = G / 64;
     const int wave = threadIdx.x >> 6;
-    if ((threadIdx.x & 63) == 0) { lds[3 * wave] = w.mx; lds[3 * wave + 1] = w.s; if (ENT) lds[3 * wave + 2] = w.sd; }
+    if ((threadIdx.x & 63) == 0) { lds[3 * wave] = w.mx; lds[3 * wave + 1] = w.s; if (ENT) lds[3 * wave + 2] = w.sy; }
     __syncthreads();
     // every 16 lanes read the (at most 16) waves' parts, one each
     const int k = threadIdx.x & 15;
@@ -83,7 +85,7 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
     if (k < NW) p = RowStat{lds[3 * k], lds[3 * k + 1], ENT ? lds[3 * k + 2] : 0.f};
     RowStat all = rebase<ENT>(p, lanes_max<16>(p.mx), c);
     all.s = lanes_sum<16>(all.s);
-    if (ENT) all.sd = lanes_sum<16>(all.sd);
+    if (ENT) all.sy = lanes_sum<16>(all.sy);
     return all;
   }
 }
@@ -91,9 +93,9 @@ __device__ __forceinline__ RowStat group_join(RowStat r, float c, float* lds) {
 // adds an element's, a piece's terms to r, whose maximum covers them
 template <bool ENT>
 __device__ __forceinline__ void add_one(RowStat& r, float x, float base, float c) {
-  const float d = x - base, e = exp2_hw(d * c);
+  const float y = (x - base) * c, e = exp2_hw(y);
   r.s += e;
-  if (ENT) r.sd += e * finite_d(d);
+  if (ENT) r.sy += e * finite_y(y);
 }
 template <class T, bool ENT>
 __device__ __forceinline__ void add_piece(RowStat& r, u32x4_t v, float base, float c) {
@@ -139,7 +141,7 @@ __device__ __forceinline__ RowOut row_out(const RowStat& r, float xt, float inv_
   RowOut o;
   o.ls = logf(r.s);
   o.logp = (xt - r.base()) * inv_t - o.ls;
-  o.ent = ent ? o.ls - r.sd / r.s * inv_t : 0.f;
+  o.ent = ent ? o.ls - r.sy / r.s * TOKEN_LN2 : 0.f;
   return o;
 }
 
@@ -167,7 +169,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void k_token_logp(RowArgs a) {
   }
 }
 
-// Few long rows: statistics of slices of a row, one block each: (max, sum e, sum e d), and in the first slice's spare place the target's
+// Few long rows: statistics of slices of a row, one block each: (max, sum e, sum e y), and in the first slice's spare place the target's
 // logit (the gradient may overwrite it in the logits' memory before every block has read it).
 template <class T, bool ENT>
 __global__ __launch_bounds__(256) void k_token_part(RowArgs a) {
@@ -178,7 +180,7 @@ __global__ __launch_bounds__(256) void k_token_part(RowArgs a) {
   const float c = a.inv_t * TOKEN_LOG2E;
   const int from = blockIdx.x * a.slice_len, n = min(a.vocab - from, a.slice_len);
   const RowStat r = group_join<256, ENT>(stream_stat<T, 256, ENT>((const T*)a.logits + row * a.ld + from, n, threadIdx.x, c), c, lds);
-  if (threadIdx.x == 0) *(float4*)(a.part + 4 * (row * a.slices + blockIdx.x)) = make_float4(r.mx, r.s, r.sd, blockIdx.x == 0 ? to_f(((const T*)a.logits)[row * a.ld + t]) : 0.f);
+  if (threadIdx.x == 0) *(float4*)(a.part + 4 * (row * a.slices + blockIdx.x)) = make_float4(r.mx, r.s, r.sy, blockIdx.x == 0 ? to_f(((const T*)a.logits)[row * a.ld + t]) : 0.f);
 }
 // the parts of a row (at most 64), joined by one wave
 template <bool ENT>
@@ -206,16 +208,23 @@ __global__ __launch_bounds__(256) void k_token_join(RowArgs a) {
   }
 }
 
-// ---- gradient: -e (k0 + k1 d), and `add` more at the target
-struct GradCoef { float mx, c, k0, k1, add; };
-// g: dL/dlogp, h: dL/dH; is = 1 / (s temperature)
-__device__ __forceinline__ GradCoef grad_coef(float g, float h, float ent, float ls, float mx, float is, float inv_t) {
-  return GradCoef{mx, inv_t * TOKEN_LOG2E, (g + h * (ent - ls)) * is, h * inv_t * is, g * inv_t};
+// ---- gradient: -e (k0 + k1 y) / temperature, at the target (g - e (k0 + k1 y)) / temperature.  Where |k| / temperature is beyond 2^100 (a
+// small temperature, a large loss scale), a power of two, 2^b, goes into e instead of the coefficients, so that neither they nor their product
+// with a y of -200 overflow and an e of 0 makes 0 of them; it costs nothing in the loops.  b = 0 otherwise.
+struct GradCoef { float mx, c, b, k0, k1, target; };   // target: the whole gradient there
+// g: dL/dlogp, h: dL/dH; is = 1 / s; xt: the target's logit
+template <bool ENT>
+__device__ __forceinline__ GradCoef grad_coef(float g, float h, float ent, float ls, float mx, float is, float inv_t, float xt) {
+  const float c = inv_t * TOKEN_LOG2E, k0 = (ENT ? g + h * (ent - ls) : g) * is, k1 = ENT ? h * TOKEN_LN2 * is : 0.f;
+  const float y = (xt - mx) * c, e = exp2_hw(y);
+  const int b = max(0, __builtin_amdgcn_frexp_expf(fmaxf(fabsf(k0), fabsf(k1))) + __builtin_amdgcn_frexp_expf(inv_t) - 100);
+  const float f = ldexpf(inv_t, -b), m0 = k0 * f, m1 = k1 * f;
+  return GradCoef{mx, c, (float)b, m0 - m1 * (float)b, m1, (g - (ENT ? e * k0 + e * finite_y(y) * k1 : e * k0)) * inv_t};
 }
 template <bool ENT>
 __device__ __forceinline__ float grad_one(float x, const GradCoef& k) {
-  const float d = x - k.mx, e = exp2_hw(d * k.c);
-  return -e * (ENT ? k.k0 + k.k1 * finite_d(d) : k.k0);
+  const float y = (x - k.mx) * k.c + k.b, e = exp2_hw(y);
+  return -e * (ENT ? k.k0 + k.k1 * finite_y(y) : k.k0);
 }
 template <class T, bool ENT>
 __device__ __forceinline__ u32x4_t grad_piece(u32x4_t v, const GradCoef& k) {
@@ -263,17 +272,17 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
     if (q.one >= 0) y[q.one] = from_f<T>(0.f);
     return;
   }
-  const float g = a.dlogp[row], h = ENT ? a.dentropy[row] : 0.f, H = ENT ? a.entropy[row] : 0.f;
-  const GradCoef k = grad_coef(g, h, H, ls, mx, expf(-ls) * a.inv_t, a.inv_t);
   // the target's element is written again, by the thread that wrote it
   const int slice = G < 256 ? 0 : blockIdx.x * (G * BACK_PIECES * N), r = t - q.head;
   const bool owner = r >= 0 && r < q.full ? r >= slice && r < slice + G * BACK_PIECES * N && (r - slice) / N % G == tid : t == q.one;
-  const float xt = owner ? to_f(x[t]) : 0.f, xl = q.one >= 0 ? to_f(x[q.one]) : 0.f;
+  const float xl = q.one >= 0 ? to_f(x[q.one]) : 0.f;
+  const float g = a.dlogp[row], h = ENT ? a.dentropy[row] : 0.f, H = ENT ? a.entropy[row] : 0.f;
+  const GradCoef k = grad_coef<ENT>(g, h, H, ls, mx, expf(-ls), a.inv_t, owner ? to_f(x[t]) : mx);
   Pieces<BACK_PIECES> v;
   each<BACK_PIECES>([&](auto u) INLINE { if (from + u * G * N < q.full) piece<u>(v) = load_piece(x + q.head + from + u * G * N); });
   each<BACK_PIECES>([&](auto u) INLINE { if (from + u * G * N < q.full) store(y + q.head + from + u * G * N, grad_piece<T, ENT>(piece<u>(v), k)); });
   if (q.one >= 0) y[q.one] = from_f<T>(grad_one<ENT>(xl, k));
-  if (owner) y[t] = from_f<T>(grad_one<ENT>(xt, k) + k.add);
+  if (owner) y[t] = from_f<T>(k.target);
 }
 
 // ---- loss
@@ -308,12 +317,13 @@ __device__ __forceinline__ LossTerm loss_term(const RowArgs& a, const LossIn& in
   return o;
 }
 // The record of a row and the coefficients of its gradient; one thread (writes) leaves the log-probability.
-__device__ __forceinline__ GradCoef loss_row(const RowArgs& a, int64_t row, const LossIn& in, const RowStat& r, float xt, bool ent, bool writes, LossRecord* rec) {
-  const RowOut o = row_out(r, xt, a.inv_t, ent);
+template <bool ENT>
+__device__ __forceinline__ GradCoef loss_row(const RowArgs& a, int64_t row, const LossIn& in, const RowStat& r, float xt, bool writes, LossRecord* rec) {
+  const RowOut o = row_out(r, xt, a.inv_t, ENT);
   const LossTerm l = loss_term(a, in, o.logp, o.ent);
   if (writes && a.logp) a.logp[row] = o.logp;
   *rec = l.rec;
-  return grad_coef(l.g, l.h, o.ent, o.ls, r.base(), a.inv_t / r.s, a.inv_t);
+  return grad_coef<ENT>(l.g, l.h, o.ent, o.ls, r.base(), 1.f / r.s, a.inv_t, xt);
 }
 template <class T>
 __device__ __forceinline__ LossRecord loss_idle(const RowArgs& a, int64_t row, T* y, int n, int tid, int G, bool writes) {
@@ -349,11 +359,11 @@ __device__ __forceinline__ LossRecord loss_in_registers(const RowArgs& a, int64_
   r = group_join<G, ENT>(r, c, lds);
   if (r.idle()) return loss_idle(a, row, y, a.vocab, tid, G, tid == 0);
   LossRecord rec;
-  const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0, &rec);
+  const GradCoef q = loss_row<ENT>(a, row, in, r, xt, tid == 0, &rec);
   each<K>([&](auto k) INLINE { if (at + k * G * N < w.full) store_piece(y + w.head + at + k * G * N, grad_piece<T, ENT>(piece<k>(v), q)); });
   if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
   // the target's element again, by the thread that wrote it with its piece
-  if (owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
+  if (owns<T, G>(w, t, tid)) y[t] = from_f<T>(q.target);
   return rec;
 }
 template <class T, int G, int K, bool ENT>
@@ -368,7 +378,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G, K >= 16 ? 4 : K == 8 ? 6 : K == 
 
 // The gradient of n elements by G threads; t: the target's place among them, if it is one of them.
 template <class T, int G, bool ENT>
-__device__ __forceinline__ void stream_gradient(const T* x, T* y, int n, int tid, const GradCoef& q, int t, float xt) {
+__device__ __forceinline__ void stream_gradient(const T* x, T* y, int n, int tid, const GradCoef& q, int t) {
   constexpr int N = Piece<T>::N, U = 4;
   const Cut w = cut_row(x, n, tid);
   const float xl = w.one >= 0 ? to_f(x[w.one]) : 0.f;
@@ -378,7 +388,7 @@ __device__ __forceinline__ void stream_gradient(const T* x, T* y, int n, int tid
     each<U>([&](auto u) INLINE { if (i + u * G * N < w.full) store_piece(y + w.head + i + u * G * N, grad_piece<T, ENT>(piece<u>(v), q)); });
   }
   if (w.one >= 0) y[w.one] = from_f<T>(grad_one<ENT>(xl, q));
-  if (t >= 0 && t < n && owns<T, G>(w, t, tid)) y[t] = from_f<T>(grad_one<ENT>(xt, q) + q.add);
+  if (t >= 0 && t < n && owns<T, G>(w, t, tid)) y[t] = from_f<T>(q.target);
 }
 
 // Longer rows: read twice by a block (2048 x 152064 this way: 294 us, 252 in registers).
@@ -403,8 +413,8 @@ __global__ __launch_bounds__(1024) void k_token_loss_long(RowArgs a) {
   LossRecord rec;
   if (r.idle()) rec = loss_idle(a, row, y, a.vocab, tid, G, tid == 0);
   else {
-    const GradCoef q = loss_row(a, row, in, r, xt, ENT, tid == 0, &rec);
-    stream_gradient<T, G, ENT>(x, y, a.vocab, tid, q, t, xt);
+    const GradCoef q = loss_row<ENT>(a, row, in, r, xt, tid == 0, &rec);
+    stream_gradient<T, G, ENT>(x, y, a.vocab, tid, q, t);
   }
   if (tid == 0) ((LossRecord*)a.record)[row] = rec;
 }
@@ -423,8 +433,8 @@ __global__ __launch_bounds__(256) void k_token_loss_slice(RowArgs a) {
   if (r.idle()) rec = loss_idle(a, row, y, n, tid, 256, first);
   else {
     const float xt = a.part[4 * row * a.slices + 3];
-    const GradCoef q = loss_row(a, row, loss_in(a, row), r, xt, ENT, first, &rec);
-    stream_gradient<T, 256, ENT>(x, y, n, tid, q, t - from, xt);
+    const GradCoef q = loss_row<ENT>(a, row, loss_in(a, row), r, xt, first, &rec);
+    stream_gradient<T, 256, ENT>(x, y, n, tid, q, t - from);
   }
   if (first) ((LossRecord*)a.record)[row] = rec;
 }

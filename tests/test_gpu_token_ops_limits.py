@@ -1,0 +1,95 @@
+"""The operators of a token policy at the ends of their ranges: temperatures and coefficients whose products leave fp32, infinite
+log-probabilities, log-ratios next to 0, masks over whole tiles, offsets that are wrong, calls recorded into a graph.
+
+Definitions, and tolerances that count roundings, are those of test_gpu_token_ops."""
+import math
+
+import pytest
+
+from paper_2509_16434_amd import learner as L
+
+from test_gpu_token_ops import TYPES, U32, gradient_definition, gradient_tolerance, rnd, row_definition, row_tolerance
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+def rows_at(temperature, rows, vocab, dtype, seed, low):
+    """Logits that differ by a few temperatures, about half of them banned with `low`; a row that the mask leaves nothing of, one that it
+    leaves one token of, an idle one."""
+    x = (torch.randn(rows, vocab, generator=rnd(seed), device="cuda") * (3 * min(temperature, 1.0))).to(dtype)
+    target = torch.randint(0, vocab, (rows,), generator=rnd(seed + 1), device="cuda").to(torch.int32)
+    ban = torch.rand(rows, vocab, generator=rnd(seed + 2), device="cuda") < 0.5
+    ban.scatter_(1, target.long()[:, None], False)
+    x.masked_fill_(ban, low)
+    x[1], x[2] = low, low
+    x[2, vocab // 2], target[2], target[3] = 0.0, vocab // 2, -1
+    return x, target
+
+
+# every width of the kernels' groups, rows in slices, rows read twice
+WIDTHS = [(5, 40), (5, 400), (5, 700), (5, 3000), (5, 9000), (5, 20000), (5, 70000), (100, 45000), (100, 210000)]
+# temperature, coefficient of the entropy, what a banned logit is: 1 / T and its square beyond fp32, e of the lowest value above 0, coefficients
+# whose product with a large negative number is infinite
+SETTINGS = [(1e-6, 1.0, "banned"), (1e-6, 1.0, "lowest"), (1e-25, 1.0, "banned"), (1e-38, 0.1, "banned"), (3e37, 1.0, "lowest"), (1.0, 1e10, "banned"), (1.0, 1e36, "lowest")]
+
+
+def vanishing(size, h, ent, temperature):
+    """exp2 gives 0 below 2^-126: what a probability below that would have added to an element."""
+    return 4 * 2.0 ** -126 * (size + h * (200 + ent.abs())[:, None]) / temperature
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("temperature,h,kind", SETTINGS)
+@pytest.mark.parametrize("rows,vocab", WIDTHS)
+def test_entropy_and_its_gradient_at_any_temperature(rows, vocab, temperature, h, kind, dtype):
+    dt = TYPES[dtype]
+    x, target = rows_at(temperature, rows, vocab, dt, vocab, -math.inf if kind == "banned" else torch.finfo(dt).min)
+    active, at, d, p, logp, ent = row_definition(x, target, temperature)
+    tol, tol_ent = row_tolerance(d, p, at, vocab)
+    got, got_ent, stat = L.token_logp(x, target, temperature=temperature, want_entropy=True)
+    assert bool(((got.double() - logp).abs() <= tol).all()) and bool(((got_ent.double() - ent).abs() <= tol_ent).all())
+    g = 0.3 * torch.randn(rows, generator=rnd(5), device="cuda")
+    for dlogp, dent in ((g, None), (g, h * torch.randn(rows, generator=rnd(6), device="cuda"))):
+        back = L.token_logp_backward(x, target, stat, dlogp, temperature=temperature, entropy=got_ent if dent is not None else None, dentropy=dent).double()
+        e = torch.zeros_like(ent) if dent is None else dent.double()
+        want, size = gradient_definition(active, at, d, p, dlogp.double(), e, ent, temperature)
+        bound = gradient_tolerance(want, size, d, tol + (dent is not None) * (tol_ent + tol), vocab, dt) + vanishing(dlogp.double().abs()[:, None], e.abs()[:, None], ent, temperature)
+        off = (back - want).abs()
+        assert bool((off <= bound).all()), (dent is not None, float((off / bound).nan_to_num(nan=math.inf).max()))
+    # the loss: nothing is clipped, so that dL/dlogp = -rho A
+    old, adv = (logp + 0.1 * torch.randn(rows, generator=rnd(7), device="cuda")).float(), 0.3 * torch.randn(rows, generator=rnd(8), device="cuda")
+    for ent_coef in (0.0, h):
+        grad, stats, _ = L.token_loss(x, target, old, adv, temperature=temperature, clip_lo=0.9, clip_hi=9.0, ent_coef=ent_coef)
+        rho = torch.where(active, (logp - old.double()).exp(), 0.0)
+        minus_h = torch.where(active, -ent_coef * torch.ones_like(ent), 0.0)
+        want, size = gradient_definition(active, at, d, p, -rho * adv.double(), minus_h, ent, temperature)
+        move = (tol + U32 * (4 * logp.abs() + 8)) * rho * adv.double().abs()
+        bound = gradient_tolerance(want, size, d, tol + (ent_coef > 0) * tol_ent, vocab, dt) + 1.01 * move[:, None] * (p + torch.zeros_like(p).scatter_(1, at, 1.0)) / temperature
+        bound = bound + vanishing((rho * adv.double().abs())[:, None], ent_coef, ent, temperature)
+        off = (grad.double() - want).abs()
+        assert bool((off <= bound).all()), (ent_coef, float((off / bound).nan_to_num(nan=math.inf).max()))
+        # a hundred entropies of 10 times 1e36 are beyond fp32: L is infinite then, and says so
+        assert stats[7].item() == (ent_coef * ent.sum().item() > torch.finfo(torch.float32).max) and (ent_coef == 0 or abs(stats[3].item() - ent.sum().item()) <= float(tol_ent.sum()) + 4 * U32 * ent.sum().item())
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", WIDTHS)
+def test_rows_of_one_token_have_no_gradient(rows, vocab, dtype):
+    """One token left: p = 1, so that every gradient is 0 whatever the coefficients and the temperature."""
+    x = torch.full((rows, vocab), -math.inf, dtype=TYPES[dtype], device="cuda")
+    target = torch.randint(0, vocab, (rows,), generator=rnd(vocab), device="cuda").to(torch.int32)
+    x.scatter_(1, target.long()[:, None], 2.5)
+    old = torch.zeros(rows, device="cuda")
+    for temperature, size in ((1.0, 1e6), (1e-3, 1e30), (6e-39, 1e9)):
+        logp, ent, stat = L.token_logp(x, target, temperature=temperature, want_entropy=True)
+        assert not bool(logp.any()) and not bool(ent.any())
+        for dent in (None, old + size):
+            assert not bool(L.token_logp_backward(x, target, stat, old + size, temperature=temperature, entropy=ent if dent is not None else None, dentropy=dent).any())
+        for ent_coef in (0.0, size):
+            if ent_coef * size > torch.finfo(torch.float32).max:   # dL/dH itself is beyond fp32: refused
+                with pytest.raises(L.LearnerError):
+                    L.token_loss(x, target, old, old + 1, scale=size, temperature=temperature, ent_coef=ent_coef)
+                continue
+            grad, stats, _ = L.token_loss(x, target, old, old + 1, scale=size, temperature=temperature, ent_coef=ent_coef)
+            assert not bool(grad.any()) and stats[7].item() == 0
