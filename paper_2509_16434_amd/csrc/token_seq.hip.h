@@ -28,7 +28,8 @@ struct PairRecord { double loss, right, margin, chosen, rejected, active; };
 __device__ __forceinline__ double pair_value(int kind, double beta, double ls, double D) {
   if (kind != 0) { const double e = D - 0.5 / beta; return e * e; }
   const double x = beta * D, soft = log1p(exp(-fabs(x)));             // -log sigmoid(|x|)
-  return (1 - ls) * (soft + (x < 0 ? -x : 0)) + ls * (soft + (x > 0 ? x : 0));
+  // a term whose weight is 0 may be infinite (D is where a token's log-probability is)
+  return (ls < 1 ? (1 - ls) * (soft + (x < 0 ? -x : 0)) : 0) + (ls > 0 ? ls * (soft + (x > 0 ? x : 0)) : 0);
 }
 __device__ __forceinline__ double pair_slope(int kind, double beta, double ls, double D) {
   return kind != 0 ? 2 * (D - 0.5 / beta) : beta * (ls - 1 / (1 + exp(beta * D)));

@@ -93,3 +93,44 @@ def test_rows_of_one_token_have_no_gradient(rows, vocab, dtype):
                 continue
             grad, stats, _ = L.token_loss(x, target, old, old + 1, scale=size, temperature=temperature, ent_coef=ent_coef)
             assert not bool(grad.any()) and stats[7].item() == 0
+
+
+@pytest.mark.parametrize("pairs", [2, 300, 2500])
+def test_pairs_of_infinite_difference(pairs):
+    """A token that its mask forbids (or the reference's does) makes a difference infinite: the loss of such a pair is 0 on the right side,
+    infinite on the wrong one, and with smoothing infinite on both; its gradient is finite, and 0 on the right side."""
+    n, beta = 3, 0.5
+    off = torch.arange(2 * pairs + 1, device="cuda") * n
+    base = -torch.rand(2 * pairs * n, generator=rnd(1), device="cuda")
+    at = pairs // 2   # the pair; its sequences begin at n * at and n * (pairs + at)
+    D = (base[:pairs * n] - base[pairs * n:]).double().view(pairs, n).sum(1)
+    others = torch.ones(pairs, dtype=torch.bool, device="cuda")
+    others[at] = False
+    for place, value, with_ref, sign in ((pairs + at, -math.inf, False, 1), (at, -math.inf, True, 1), (at, -math.inf, False, -1)):
+        logp, ref = base.clone(), torch.zeros_like(base) if with_ref else None
+        (ref if with_ref else logp)[n * place + 1] = value
+        for ls in (0.0, 1.0, 0.25):
+            grad, margin, stats = L.pair_loss(logp, off, logp_ref=ref, beta=beta, label_smoothing=ls, scale=1.0 / pairs)
+            soft = torch.nn.functional.softplus
+            rest = ((1 - ls) * soft(-beta * D) + ls * soft(beta * D))[others].sum().item() / pairs
+            finite = (sign > 0 and ls == 0) or (sign < 0 and ls == 1)
+            assert margin[at].item() == sign * math.inf and stats[6].item() == (not finite)
+            # 64 bits inside; scale and the result are rounded once each
+            assert abs(stats[0].item() - rest) <= 4 * U32 * rest if finite else stats[0].item() == math.inf
+            slope = beta * (ls - (sign < 0)) / pairs
+            mine = torch.cat([grad[n * at:n * (at + 1)], -grad[n * (pairs + at):n * (pairs + at + 1)]])
+            assert bool(torch.isfinite(grad).all()) and bool(((mine - slope).abs() <= 4 * U32 * abs(slope)).all())
+
+
+def test_a_forbidden_token_in_a_rejected_answer():
+    """The whole chain: log-probability -infinity, a pair on its right side, and a gradient of the logits without NaN."""
+    x = torch.randn(6, 50, generator=rnd(3), device="cuda")
+    x[4, 7] = -math.inf
+    target = torch.tensor([1, 2, 3, 4, 7, 6], dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 2, 3, 4, 6], dtype=torch.int64, device="cuda")   # chosen 0, 1; rejected 2, 3 (of two tokens)
+    logp, _, stat = L.token_logp(x, target)
+    dlogp, margin, stats = L.pair_loss(logp, off, beta=0.3)
+    D = (logp[0] + logp[1] - logp[3]).item()
+    assert stats[6].item() == 0 and margin[1].item() == math.inf and abs(stats[0].item() - math.log1p(math.exp(-0.3 * D))) <= 1e-6
+    d = L.token_logp_backward(x, target, stat, dlogp)
+    assert bool(torch.isfinite(d).all()) and not bool(d[2].any()) and not bool(d[4:].any()) and bool(d[0].any())
