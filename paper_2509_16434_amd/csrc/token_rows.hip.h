@@ -286,8 +286,20 @@ __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {
 }
 
 // ---- loss
-// exp d - 1 - d from exp d - 1, a small difference near 0; where exp d is infinite (or d below all its digits), it is that
-__device__ __forceinline__ float less_linear(float em, float d) { return d < 80.f ? em - d : em; }
+// exp d - 1 - d, em being exp d - 1.  Near 0 their difference loses what the result is made of (d = 2^-12: all but 12 bits, and the sign with
+// the last of them), so there it is the series up to d^9 / 9! (the next term is 2^-29 of the sum at 1/2); where exp d is infinite (or d below
+// all its digits), it is that.  12 roundings at the most, at +-1/2.
+__device__ __forceinline__ float less_linear(float em, float d) {
+  float q = 1.f / 362880;
+  q = fmaf(q, d, 1.f / 40320);
+  q = fmaf(q, d, 1.f / 5040);
+  q = fmaf(q, d, 1.f / 720);
+  q = fmaf(q, d, 1.f / 120);
+  q = fmaf(q, d, 1.f / 24);
+  q = fmaf(q, d, 1.f / 6);
+  q = fmaf(q, d, 0.5f);
+  return fabsf(d) < 0.5f ? q * d * d : d < 80.f ? em - d : em;
+}
 // What a token adds to the loss (its record) and the derivatives of that by logp (g) and H (h).
 struct LossTerm { float g, h; LossRecord rec; };
 struct LossIn { float old, ref, adv, w; };

@@ -134,3 +134,33 @@ def test_a_forbidden_token_in_a_rejected_answer():
     assert stats[6].item() == 0 and margin[1].item() == math.inf and abs(stats[0].item() - math.log1p(math.exp(-0.3 * D))) <= 1e-6
     d = L.token_logp_backward(x, target, stat, dlogp)
     assert bool(torch.isfinite(d).all()) and not bool(d[2].any()) and not bool(d[4:].any()) and bool(d[0].any())
+
+
+@pytest.mark.parametrize("size", [0.0, 2.0 ** -20, 2.0 ** -12, 2.0 ** -7, 0.1, 0.6, 3.0, 20.0])
+@pytest.mark.parametrize("rows,vocab", [(1, 30), (100, 300), (300, 3000), (5, 70000)])
+def test_estimates_from_log_ratios_next_to_0(rows, vocab, size):
+    """exp x - 1 - x is positive for every x but 0, and keeps its digits: 12 roundings of fp32 of every term.  (exp x - 1 and x are off by one
+    and a half and no roundings of about |x|, the result is about x^2 / 2; so the difference of the two is not enough below |x| = 1/2, and has
+    lost a factor of 10 there.)"""
+    x = torch.randn(rows, vocab, generator=rnd(1), device="cuda")
+    target = torch.randint(0, vocab, (rows,), generator=rnd(2), device="cuda").to(torch.int32)
+    zero = torch.zeros(rows, device="cuda")
+    logp = L.token_loss(x, target, zero, zero)[2]
+    far = size * torch.randn(rows, generator=rnd(3), device="cuda")
+    old, ref = logp - far, logp + far
+    weight = torch.rand(rows, generator=rnd(4), device="cuda") + 0.5
+    stats, again = L.token_loss(x, target, old, zero, logp_ref=ref, weight=weight)[1:]
+    assert torch.equal(again, logp)
+
+    def estimate(d):
+        """In 64 bits: the series where the difference loses digits."""
+        term, total = d * d / 2, torch.zeros_like(d)
+        for k in range(3, 20):
+            total, term = total + term, term * d / k
+        return torch.where(d.abs() < 0.5, total, torch.expm1(d) - d)
+
+    # the differences that are taken, as fp32 has them (exact where the two are within a factor of two of one another)
+    lr, d = (logp - old).double(), (ref - logp).double()
+    want_kl, want_old = (weight.double() * estimate(d)).sum().item(), estimate(lr).mean().item()
+    for got, want in ((stats[2].item(), want_kl), (stats[4].item(), want_old)):
+        assert abs(got - want) <= 13 * U32 * want and (got > 0) == (want > 0), (got, want)
