@@ -206,6 +206,10 @@ at::Tensor out_matrix(PyObject* o, const at::Tensor& like) {
   if (t.sizes() != like.sizes() || t.scalar_type() != like.scalar_type()) throw Wrong{PyExc_ValueError, "out: expected the shape and type of the input"};
   return t;
 }
+// `out` has been written: autograd is to know it, for a backward pass that needs what was there.
+void changed(PyObject* out, const at::Tensor& t) {
+  if (out != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // Memory of `out` and of an input: apart, the same place with the same row stride, or side by side in rows of one stride.
 void apart_or_same(const at::Tensor& out, int64_t ldo, const at::Tensor& in, int64_t ldi, const char* name) {
   if (!in.defined() || !out.numel()) return;
@@ -292,6 +296,7 @@ PyObject* py_dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
     apart_or_same(y, ldy, x, ldx, "x");
     apart_or_same(y, ldy, res, ldr, "residual");
     const int rc = without_lock([&] { return f_dropout(dt, rows, cols, x.data_ptr(), ldx, ptr<const int64_t>(ids), ptr<void>(res), ldr, p, seed, layer, y.data_ptr(), ldy, st); });
+    if (rc == PPO_OK) changed(a[7], y);
     return Py_BuildValue("iN", rc, wrap(std::move(y)));
   });
 }
@@ -338,6 +343,7 @@ PyObject* py_token_logp_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return f_token_logp_backward(dt, rows, V, x.data_ptr(), ld, ptr<const int32_t>(target), (float)temperature, ptr<const float>(stat), ptr<const float>(dlogp),
                                    ptr<const float>(entropy), ptr<const float>(dentropy), d.data_ptr(), ldd, st);
     });
+    if (rc == PPO_OK) changed(a[8], d);
     return Py_BuildValue("iN", rc, wrap(std::move(d)));
   });
 }
@@ -367,6 +373,7 @@ PyObject* py_token_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
       return f_token_loss(dt, rows, V, x.data_ptr(), ld, ptr<const int32_t>(target), ptr<const float>(old), ptr<const float>(ref), ptr<const float>(adv), ptr<const float>(weight),
                           &hp, d.data_ptr(), ldd, ptr<float>(logp), ptr<float>(stats), ptr<void>(ws), wsb, st);
     });
+    if (rc == PPO_OK) changed(a[13], d);
     return Py_BuildValue("iNNN", rc, wrap(std::move(d)), wrap(std::move(stats)), wrap(std::move(logp)));
   });
 }

@@ -242,6 +242,8 @@ def permutation_static(S: int, seed: int, update_idx: int, epoch: int, out=None,
 # ---- operators of a policy that answers in tokens (include/ppo_learner.h has the formulas).  They take CUDA tensors and allocate
 # their results with torch; a matrix may have any row stride.  Work runs on the device of the tensors, on `stream`: None is torch's
 # current stream of that device, and with another one the results belong to it (inputs must be ready on it, as with any stream).
+# They stand outside autograd: inputs that require a gradient are taken as they are, results carry no history (a gradient of the logits goes
+# on with logits.backward(dlogits)), and `out` counts as a change in place of its tensor.
 
 def _on_stream(first, stream, call, *args):
     if not isinstance(first, torch.Tensor) or not first.is_cuda:

@@ -164,3 +164,28 @@ def test_estimates_from_log_ratios_next_to_0(rows, vocab, size):
     want_kl, want_old = (weight.double() * estimate(d)).sum().item(), estimate(lr).mean().item()
     for got, want in ((stats[2].item(), want_kl), (stats[4].item(), want_old)):
         assert abs(got - want) <= 13 * U32 * want and (got > 0) == (want > 0), (got, want)
+
+
+def test_a_result_in_the_memory_of_a_saved_tensor_is_noticed():
+    """`out` is a change of its tensor that autograd sees: a backward pass that needs what it held fails instead of using the gradient in its
+    place."""
+    t, z = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    for call in (lambda x: L.dropout(x, 0.5, 1, out=x), lambda x: L.token_loss(x, t, z, z + 1, out=x)[0], lambda x: L.token_logp_backward(x, t, L.token_logp(x, t)[2], z + 1, out=x)):
+        leaf = torch.randn(4, 8, device="cuda", requires_grad=True)
+        x = leaf.exp()   # its backward pass multiplies by x
+        before = x._version
+        out = call(x)
+        assert out is x and x._version > before
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            x.sum().backward()
+    # results of their own: nothing of the inputs' history changes, and none is theirs
+    leaf = torch.randn(4, 8, device="cuda", requires_grad=True)
+    x = leaf.exp()
+    d = L.token_loss(x, t, z, z + 1)[0]
+    assert not d.requires_grad
+    x.backward(d)
+    assert torch.equal(leaf.grad, d * x.detach())
+    with torch.inference_mode():   # no versions there
+        x = torch.randn(4, 8, device="cuda")
+        assert L.dropout(x, 0.5, 1, out=x) is x
+    assert L.dropout(x, 0.5, 1, out=torch.empty(4, 8, device="cuda")).shape == (4, 8)
