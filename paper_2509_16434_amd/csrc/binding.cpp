@@ -3,6 +3,7 @@
 // Python attributes and calling through ctypes cost 3.4 us beside the kernel launch behind it, which set the pace of
 // small tasks (64 environments: 16 writes, 145 .. 161 -> 110 .. 114 us).  Marshalling only: the library's functions are
 // handed in as addresses by learner.py, which loads the library and binds everything else.
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ATen.h>
 #include <c10/core/DeviceGuard.h>
@@ -257,8 +258,8 @@ PyObject* guarded(F body) {
     return body();
   } catch (const Wrong& w) {
     if (w.type) PyErr_SetString(w.type, w.text.c_str());
-  } catch (const std::exception& e) {
-    PyErr_SetString(PyExc_RuntimeError, e.what());
+  } catch (const std::exception&) {
+    torch::translate_exception_to_python(std::current_exception());   // as torch's own functions tell it, OutOfMemoryError among others
   }
   return nullptr;
 }

@@ -189,3 +189,16 @@ def test_a_result_in_the_memory_of_a_saved_tensor_is_noticed():
         x = torch.randn(4, 8, device="cuda")
         assert L.dropout(x, 0.5, 1, out=x) is x
     assert L.dropout(x, 0.5, 1, out=torch.empty(4, 8, device="cuda")).shape == (4, 8)
+
+
+def test_no_memory_is_torchs_error():
+    """A result that does not fit is torch's own OutOfMemoryError, as a caller who retries with less expects."""
+    torch.cuda.empty_cache()
+    x = torch.zeros((torch.cuda.memory_reserved() >> 8) + (1 << 20), 64, device="cuda")   # larger than all that may be free inside what others hold
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (64 << 20)) / torch.cuda.get_device_properties(0).total_memory)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            L.dropout(x, 0.5, 1)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert L.dropout(x, 0.5, 1).shape == x.shape
