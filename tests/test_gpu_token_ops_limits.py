@@ -2,13 +2,14 @@
 log-probabilities, log-ratios next to 0, masks over whole tiles, offsets that are wrong, calls recorded into a graph.
 
 Definitions, and tolerances that count roundings, are those of test_gpu_token_ops."""
+import ctypes as C
 import math
 
 import pytest
 
 from paper_2509_16434_amd import learner as L
 
-from test_gpu_token_ops import TYPES, U32, gradient_definition, gradient_tolerance, rnd, row_definition, row_tolerance
+from test_gpu_token_ops import TYPES, U32, everything_inputs, gradient_definition, gradient_tolerance, rnd, row_definition, row_tolerance
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -202,3 +203,96 @@ def test_no_memory_is_torchs_error():
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert L.dropout(x, 0.5, 1).shape == x.shape
+
+
+# ------------------------------------------------------------------------------------------ the C calls, on the caller's arrays
+
+class Guarded:
+    """An array between two others that nobody may write: everything holds the byte 0x5A first."""
+
+    def __init__(self, n, dtype=torch.float32):
+        size = n * torch.empty(0, dtype=dtype).element_size()
+        self.whole = torch.full((4096 + -(-size // 256) * 256 + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+        self.size, self.inner = size, self.whole[4096:4096 + size].view(dtype)
+
+    def ptr(self):
+        return self.inner.data_ptr()
+
+    def intact(self):
+        return bool((self.whole[:4096] == 0x5A).all()) and bool((self.whole[4096 + self.size:] == 0x5A).all())
+
+
+def ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def c_calls(x, target, old, ref, adv, off, mask, hidden, ids, stream, made):
+    """One call of every operator into arrays made before (the first time: into `made`); the results."""
+    rows, V = x.shape
+    cols, ld, seqs, lib = hidden.shape[1], x.stride(0), off.numel() - 1, L._lib
+    sizes = dict(logp=rows, ent=rows, stat=2 * rows, d=rows * V, dl=rows * V, loss_stats=8, loss_logp=rows, dlogp=rows, margin=seqs // 2, pair_stats=7, adv=rows, ret=rows, y=rows * cols)
+    ws = dict(ws_logp=lib.ppo_token_logp_ws_bytes(rows, V), ws_loss=lib.ppo_token_loss_ws_bytes(rows, V), ws_pair=lib.ppo_pair_ws_bytes(seqs // 2, rows),
+              ws_gae=lib.ppo_token_gae_ws_bytes(seqs, rows))
+    if not made:
+        made.update({k: Guarded(n, x.dtype if k in ("d", "dl") else hidden.dtype if k == "y" else torch.float32) for k, n in sizes.items()})
+        made.update({k: Guarded(n, torch.uint8) for k, n in ws.items()})
+    o = {k: g.ptr() for k, g in made.items()}
+    code, thp, php = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}, L.TokenHParams(1.0, 0.2, 0.2, 0.1, 0.01, 1.0), L.PairHParams(0, 0, 0.1, 0.0, 1.0)
+    for rc in (
+            lib.ppo_token_logp(code[x.dtype], rows, V, ptr(x), ld, ptr(target), 1.0, o["logp"], o["ent"], o["stat"], o["ws_logp"], ws["ws_logp"], stream),
+            lib.ppo_token_logp_backward(code[x.dtype], rows, V, ptr(x), ld, ptr(target), 1.0, o["stat"], ptr(adv), o["ent"], ptr(old), o["d"], V, stream),
+            lib.ppo_token_loss(code[x.dtype], rows, V, ptr(x), ld, ptr(target), ptr(old), ptr(ref), ptr(adv), None, C.byref(thp), o["dl"], V, o["loss_logp"], o["loss_stats"],
+                               o["ws_loss"], ws["ws_loss"], stream),
+            lib.ppo_pair_loss(seqs // 2, rows, o["logp"], ptr(ref), ptr(mask), ptr(off), C.byref(php), o["dlogp"], o["margin"], o["pair_stats"], o["ws_pair"], ws["ws_pair"], stream),
+            lib.ppo_token_gae(seqs, rows, ptr(adv), ptr(old), ptr(mask), ptr(off), None, 0.99, 0.95, o["adv"], o["ret"], o["ws_gae"], ws["ws_gae"], stream),
+            lib.ppo_dropout(code[hidden.dtype], rows, cols, ptr(hidden), cols, ptr(ids), ptr(hidden), cols, 0.3, 5, 0, o["y"], cols, stream)):
+        assert rc == 0, lib.ppo_last_error(None)
+    return [made[k].inner for k in sizes]
+
+
+@pytest.mark.parametrize("rows,vocab", [(30, 200), (300, 3000), (6, 50000), (9000, 40)])
+def test_the_c_calls_while_a_graph_is_recorded(rows, vocab):
+    """The library's calls alone between the beginning and the end of a recording, which an allocation or a synchronisation ends with an
+    error; every replay, with new inputs and eager work between, gives what an eager call gives; nothing beside the results and workspaces,
+    which are of the sizes asked for, is written."""
+    held = [a.clone() for a in everything_inputs(20, rows, vocab)]
+    made, side, graph = {}, torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c_calls(*held, side.cuda_stream, made)   # the results are allocated here, not in the recording
+    side.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        outs = c_calls(*held, side.cuda_stream, made)
+    for turn in range(3):
+        fresh, eager = everything_inputs(30 + turn, rows, vocab), {}
+        want = c_calls(*fresh, torch.cuda.current_stream().cuda_stream, eager)
+        for a, b in zip(held, fresh):
+            a.copy_(b)
+        for o in outs:
+            o.view(torch.uint8).fill_(0xA5)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(outs, want)), turn
+        assert all(g.intact() for d in (made, eager) for g in d.values())
+
+
+# offsets as a program error leaves them: outside the tokens, decreasing, all at one end
+WRONG = {"outside": lambda T, n: [-(1 << 40)] + [T // 2] * (n - 1) + [1 << 50], "decreasing": lambda T, n: [T - k * T // (n + 1) for k in range(n + 1)],
+         "to and fro": lambda T, n: [(k * 7919) % (T + 1) for k in range(n + 1)], "behind": lambda T, n: [T + 1 + k for k in range(n + 1)],
+         "before": lambda T, n: [k - n - 1 for k in range(n + 1)], "ends swapped": lambda T, n: [T] + [k * T // n for k in range(1, n)] + [0]}
+
+
+@pytest.mark.parametrize("kind", WRONG)
+@pytest.mark.parametrize("T,seqs", [(1, 2), (100, 2), (5003, 8), (70001, 600), (70001, 5000)])
+def test_wrong_offsets_write_nothing_beside_the_results(kind, T, seqs):
+    logp, last = torch.randn(T, generator=rnd(1), device="cuda"), torch.randn(seqs, generator=rnd(2), device="cuda")
+    off, lib = torch.tensor(WRONG[kind](T, seqs), dtype=torch.int64, device="cuda"), L._lib
+    stream, hp = torch.cuda.current_stream().cuda_stream, L.PairHParams(0, 1, 0.1, 0.0, 1.0)
+    g = {k: Guarded(n) for k, n in dict(dlogp=T, margin=seqs // 2, stats=7, adv=T, ret=T).items()}
+    sizes = lib.ppo_pair_ws_bytes(seqs // 2, T), lib.ppo_token_gae_ws_bytes(seqs, T)
+    g["ws"], g["ws2"] = (Guarded(n, torch.uint8) for n in sizes)
+    assert lib.ppo_pair_loss(seqs // 2, T, ptr(logp), None, None, ptr(off), C.byref(hp), g["dlogp"].ptr(), g["margin"].ptr(), g["stats"].ptr(), g["ws"].ptr(), sizes[0], stream) == 0
+    assert lib.ppo_token_gae(seqs, T, ptr(logp), ptr(logp), None, ptr(off), ptr(last), 0.9, 0.8, g["adv"].ptr(), g["ret"].ptr(), g["ws2"].ptr(), sizes[1], stream) == 0
+    torch.cuda.synchronize()
+    assert all(a.intact() for a in g.values())
+    assert all(bool(torch.isfinite(g[k].inner).all()) for k in ("margin", "stats", "adv", "ret"))
