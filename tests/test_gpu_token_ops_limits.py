@@ -296,3 +296,50 @@ def test_wrong_offsets_write_nothing_beside_the_results(kind, T, seqs):
     torch.cuda.synchronize()
     assert all(a.intact() for a in g.values())
     assert all(bool(torch.isfinite(g[k].inner).all()) for k in ("margin", "stats", "adv", "ret"))
+
+
+# ------------------------------------------------------------------------------------------------ masks over whole tiles
+
+TILE = 2048   # tokens that a block of the advantages takes
+
+
+def tile_masks(T, longest):
+    """What a mask may leave of the tiles: runs of wholly masked tiles (the longest of `longest`), stretches with one token a tile, a stretch
+    without a mask, and between them two tokens in five."""
+    g = rnd(T)
+    keep = torch.rand(T, generator=g, device="cuda") < 0.4
+    keep[:700], keep[2 * TILE:5 * TILE + 17] = True, False
+    single = torch.arange(7 * TILE + 1033, min(T, 20 * TILE), TILE, device="cuda")
+    keep[7 * TILE:20 * TILE] = False
+    keep[single] = True
+    keep[22 * TILE:24 * TILE] = True
+    keep[25 * TILE + 5:(25 + longest) * TILE + 9] = False
+    return keep
+
+
+@pytest.mark.parametrize("lengths,longest", [([60000], 3), ([5 * TILE + 20, 1, 25 * TILE, 0, 7 * TILE], 4), ([900001], 300), ([300000, 0, 700000, 5], 257), ([9000001], 1100),
+                                             ([70000, 8600000, 400000], 2500)])
+def test_advantages_across_masked_tiles(lengths, longest):
+    """Values and advantages pass through tiles that the mask leaves nothing or one token of: the recurrence between one unmasked token and
+    the next, each advantage rounded once, and the boundary values behind the last ones."""
+    off = torch.tensor([0] + lengths, device="cuda").cumsum(0)
+    T, g = int(off[-1]), rnd(len(lengths))
+    keep = tile_masks(T, longest)
+    r, v = 0.1 * torch.randn(T, generator=g, device="cuda"), torch.randn(T, generator=g, device="cuda")
+    r[~keep], v[~keep] = math.nan, math.inf
+    last = torch.randn(len(lengths), generator=g, device="cuda")
+    at = torch.cat([off.new_zeros(1), keep.cumsum(0)])[off]   # the sequences' bounds among the unmasked tokens
+    rk, vk = r[keep].double(), v[keep].double()
+    nonempty = at[1:] > at[:-1]
+    tails = (at[1:] - 1)[nonempty]
+    v_after = torch.cat([vk[1:], vk[:1]])
+    v_after[tails] = last.double()[nonempty]
+    for gamma, lam in ((0.9999, 1.0), (0.99, 0.95), (0.9, 0.0), (1.0, 1.0), (0.0, 0.7)):
+        adv, ret = L.token_gae(r, v, off, gamma, lam, last_value=last, mask=keep.to(torch.uint8))
+        assert not bool(adv[~keep].any()) and not bool(ret[~keep].any())
+        a, b = adv[keep].double(), ret[keep].double()
+        after = torch.cat([a[1:], a[:1]])
+        after[tails] = 0.0
+        rest = a - (rk + gamma * v_after - vk + gamma * lam * after)
+        assert bool((rest.abs() <= 1.01 * U32 * (a.abs() + after.abs()) + 1e-10).all()), (gamma, lam, float(rest.abs().max()))
+        assert bool(((b - a - vk).abs() <= 1.01 * U32 * (b.abs() + a.abs()) + 1e-10).all())
