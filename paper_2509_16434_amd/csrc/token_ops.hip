@@ -306,8 +306,14 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
       with_flag(hp->ent_coef != 0.f, [&](auto ent) {
         using T = decltype(t);
         constexpr bool ENT = decltype(ent)::value;
-        if (vocab <= 16 * 4 * Piece<T>::N) hipLaunchKernelGGL((k_token_loss_small<T, 4, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
-        else hipLaunchKernelGGL((k_token_loss_small<T, 8, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
+        constexpr int HOLDS = 16 * 4 * Piece<T>::N;   // logits that 16 threads hold in four pieces each
+        if constexpr (HOLDS < SMALL_VOCAB) {
+          if (vocab > HOLDS) {
+            hipLaunchKernelGGL((k_token_loss_small<T, 8, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
+            return;
+          }
+        }
+        hipLaunchKernelGGL((k_token_loss_small<T, 4, ENT>), dim3(1), dim3(1024), 0, st, a, d_stats);
       });
     });
     LAUNCHCHK("k_token_loss_small");
