@@ -95,7 +95,7 @@ int64_t parts_bytes(int64_t rows, int64_t vocab, int64_t most_rows) {
   const int s = slices_of(std::max<int64_t>(rows, 1), vocab, most_rows);
   return s > 1 ? rows * s * 16 : 0;
 }
-bool small_loss(int64_t rows, int64_t vocab) { return rows <= SMALL_ROWS && vocab <= SMALL_VOCAB; }
+bool small_loss(int64_t rows, int64_t vocab) { return rows <= SMALL_ROWS && vocab <= SMALL_VOCAB && rows * vocab <= SMALL_LOGITS; }
 int stats_blocks(int64_t rows) { return (int)std::max<int64_t>(1, std::min<int64_t>(cdiv(rows, STATS_ROWS), 1024)); }
 int64_t stats_offset(int64_t rows, int64_t vocab) {
   return (parts_bytes(rows, vocab, SLICED_LOSS_ROWS) + rows * (int64_t)sizeof(LossRecord) + 15) / 16 * 16;

@@ -486,9 +486,11 @@ __global__ __launch_bounds__(1024) void k_token_stats_join(int blocks, float kl_
   if (threadIdx.x == 0) write_stats(v, kl_coef, ent_coef, stats);
 }
 
-// A few short rows by one block, statistics included (64 rows a turn): one launch and no workspace where these are what a call costs
-// (4 rows of 64: 10.3 -> 6.5 us a call).
-constexpr int SMALL_ROWS = 128, SMALL_VOCAB = 512;
+// A few short rows by one block, statistics included (64 rows a turn): one launch and no workspace where these are what a call costs.
+// us a call among others, this way and with two launches: 4 x 64 6.5 and 10.5, 32 x 512 6.5 and 10.5, 64 x 256 7.0 and 10.6, 128 x 128 8.6 and
+// 10.5; 64 x 512 8.9 and 10.5, 128 x 256 10.3 and 10.5, 128 x 512 14.3 and 10.6.  A call alone takes 18.0 and 20.8 (16 x 512),
+// 21.6 and 20.8 (128 x 128), 22.0 and 20.7 (64 x 512).
+constexpr int SMALL_ROWS = 128, SMALL_VOCAB = 512, SMALL_LOGITS = 16384;
 template <class T, int K, bool ENT>
 __global__ __launch_bounds__(1024) void k_token_loss_small(RowArgs a, float* stats) {
   __shared__ double lds[6 * 16];

@@ -9,6 +9,8 @@ import pytest
 
 from paper_2509_16434_amd import learner as L
 
+from test_gpu_token_ops import test_token_logp_backward as check_token_logp_backward
+from test_gpu_token_ops import test_token_loss as check_token_loss
 from test_gpu_token_ops import TYPES, U32, everything_inputs, gradient_definition, gradient_tolerance, rnd, row_definition, row_tolerance
 
 pytestmark = pytest.mark.gpu
@@ -343,3 +345,13 @@ def test_advantages_across_masked_tiles(lengths, longest):
         rest = a - (rk + gamma * v_after - vk + gamma * lam * after)
         assert bool((rest.abs() <= 1.01 * U32 * (a.abs() + after.abs()) + 1e-10).all()), (gamma, lam, float(rest.abs().max()))
         assert bool(((b - a - vk).abs() <= 1.01 * U32 * (b.abs() + a.abs()) + 1e-10).all())
+
+
+# ------------------------------------------------------------------------------------------- both sides of the rules' borders
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,vocab", [(32, 512), (33, 512), (64, 256), (65, 256), (128, 128), (128, 129), (129, 128), (128, 512), (64, 512)])
+def test_loss_in_one_launch_and_in_two(rows, vocab, dtype):
+    """At most 16384 logits in at most 128 rows are one launch."""
+    assert (L._lib.ppo_token_loss_ws_bytes(rows, vocab) == 0) == (rows <= 128 and rows * vocab <= 16384)
+    check_token_loss(rows, vocab, dtype)
