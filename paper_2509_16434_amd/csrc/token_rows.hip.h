@@ -245,10 +245,13 @@ __device__ __forceinline__ void zero_row(T* y, int n, int tid, int G) {
 
 // Gradient of the log-probability and the entropy from the row's statistics: every piece by itself.  A group of G threads does a
 // slice of G BACK_PIECES pieces of a row: blockIdx.x the slice (G < 256: the row is one slice), blockIdx.y and z the row.
-// PAST: stored past the caches, for gradients that are larger than the last-level cache: they would only push out the logits, which the
-// forward pass has just read (gradient of 524 MB, 32 bits: forward and backward 311 -> 267 us).  Smaller ones are read from that cache by
-// whatever comes next (65 MB: 46 us with that reader, 50 past the caches).
-constexpr int64_t PAST_BYTES = 256000000;
+// PAST: stored past the caches, for gradients that would push out of the last-level cache (256 MB) the logits that the forward pass has
+// just read.  us of log-probability and backward pass, and with one more kernel that reads the gradient, into and past the caches:
+//   rows of 32000 bf16   128 MB 60 and 60 (106, 105), 160 MB 78 and 74 (149, 136), 250 MB 139 and 111 (233, 215), 512 MB 287 and 252 (464, 446)
+//   rows of 2000 bf16    128 MB 59 and 61 (108, 105), 160 MB 77 and 74 (146, 134), 250 MB 138 and 111 (231, 210)
+//   rows of 500 bf16     128 MB 60 and 69 (107, 115), 160 MB 79 and 86 (150, 146), 250 MB 136 and 132 (229, 235), 520 MB 302 and 324 (483, 515)
+// (the last begin inside cache lines, which two rows then write in part).  Smaller ones are worth more in the cache: 64 MB 32 and 33 (51, 54).
+constexpr int64_t PAST_BYTES = 144000000;
 constexpr int BACK_PIECES = 4;   // pieces per thread
 template <class T, int G, bool ENT, bool PAST>
 __global__ __launch_bounds__(256) void k_token_logp_backward(RowArgs a) {

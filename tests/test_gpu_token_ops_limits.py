@@ -355,3 +355,10 @@ def test_loss_in_one_launch_and_in_two(rows, vocab, dtype):
     """At most 16384 logits in at most 128 rows are one launch."""
     assert (L._lib.ppo_token_loss_ws_bytes(rows, vocab) == 0) == (rows <= 128 and rows * vocab <= 16384)
     check_token_loss(rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1098, 65536, "bf16"), (1099, 65536, "fp16"), (2197, 16384, "fp32"), (2198, 16384, "fp32"), (140000, 513, "bf16"), (140800, 512, "bf16")])
+def test_gradients_into_and_past_the_caches(rows, vocab, dtype):
+    """Gradients of 144 MB and a little less and more."""
+    assert abs(rows * vocab * torch.empty(0, dtype=TYPES[dtype]).element_size() / 144e6 - 1) < 3e-3
+    check_token_logp_backward(rows, vocab, dtype)
