@@ -75,9 +75,12 @@ int check_sizes(int32_t dtype, int64_t rows, int64_t vocab) {
 }
 
 // Rows in slices (k_token_part and what follows it): long rows that would leave part of the chip idle.  One more launch, 2 us, buys
-// the other CUs' arithmetic: 16 rows of 128000 take 8 us in slices and 13 whole (loss: 14 and 18), 200 rows 14 and 17 (loss: 31 and 25),
-// 16 rows of 32000 9 and 7 (14 and 11).
-constexpr int MAX_SLICES = 64, SLICED_ROWS = 255, SLICED_LOSS_ROWS = 96;
+// the other CUs' arithmetic.  us a call in slices and whole (log-probability by blocks of 256 threads), among others:
+//   log-probability, bf16   16 x 50000 11 and 8, 16 x 100000 11 and 12, 16 x 128000 10 and 15, 255 x 128000 16 and 19, 400 x 128000 22 and 22
+//   loss, bf16              16 x 50000 14 and 12, 16 x 128000 14 and 19, 96 x 100000 16 and 18, 128 x 100000 17 and 19, 200 x 128000 30 and 24
+//   loss, fp32              16 x 100000 14 and 16, 64 x 100000 16 and 18, 80 x 100000 20 and 19, 96 x 100000 24 and 20, 80 x 160000 30 and 31
+// A call alone, 20 to 30 us, gains from 41000 (loss) and 50000 logits (log-probability) on: 16 x 50000 23 and 25, 20.5 and 20.6.
+constexpr int MAX_SLICES = 64, SLICED_ROWS = 255, SLICED_LOSS_ROWS = 96, SLICED_LOSS_ROWS_FP32 = 72;
 int slices_of(int64_t rows, int64_t vocab, int64_t most_rows) {
   if (rows > most_rows || vocab <= 40960) return 1;
   return (int)std::min<int64_t>(std::min<int64_t>(cdiv(1024, rows), cdiv(vocab, 4096)), MAX_SLICES);
@@ -89,8 +92,8 @@ void set_slices(RowArgs& a, int64_t most_rows) {
   a.slices = (int32_t)cdiv(a.vocab, a.slice_len);
 }
 
-// Workspace of a call on rows: parts of the slices (16 bytes each); for the loss then the rows' records and the sums of the blocks that
-// add those up, or nothing where one block does it all.
+// Workspace of a call on rows: parts of the slices (16 bytes each; enough for any type); for the loss then the rows' records and the sums of
+// the blocks that add those up, or nothing where one block does it all.
 int64_t parts_bytes(int64_t rows, int64_t vocab, int64_t most_rows) {
   const int s = slices_of(std::max<int64_t>(rows, 1), vocab, most_rows);
   return s > 1 ? rows * s * 16 : 0;
@@ -320,7 +323,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
     return PPO_OK;
   }
   if (rows > 0) {
-    set_slices(a, SLICED_LOSS_ROWS);
+    set_slices(a, dtype == 0 ? SLICED_LOSS_ROWS_FP32 : SLICED_LOSS_ROWS);
     a.part = (float*)d_ws;
     a.record = (float*)d_ws + (a.slices > 1 ? rows * a.slices * 4 : 0);
     with_type(dtype, [&](auto t) {

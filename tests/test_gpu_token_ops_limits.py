@@ -252,7 +252,7 @@ def c_calls(x, target, old, ref, adv, off, mask, hidden, ids, stream, made):
     return [made[k].inner for k in sizes]
 
 
-@pytest.mark.parametrize("rows,vocab", [(30, 200), (300, 3000), (6, 50000), (9000, 40)])
+@pytest.mark.parametrize("rows,vocab", [(30, 200), (128, 512), (300, 3000), (6, 50000), (9000, 40)])
 def test_the_c_calls_while_a_graph_is_recorded(rows, vocab):
     """The library's calls alone between the beginning and the end of a recording, which an allocation or a synchronisation ends with an
     error; every replay, with new inputs and eager work between, gives what an eager call gives; nothing beside the results and workspaces,
@@ -362,3 +362,10 @@ def test_gradients_into_and_past_the_caches(rows, vocab, dtype):
     """Gradients of 144 MB and a little less and more."""
     assert abs(rows * vocab * torch.empty(0, dtype=TYPES[dtype]).element_size() / 144e6 - 1) < 3e-3
     check_token_logp_backward(rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows", [72, 73, 96, 97])
+def test_loss_of_rows_in_slices_and_whole(rows, dtype):
+    """72 rows of 32 bits and 96 of 16 are the most that are cut into slices."""
+    check_token_loss(rows, 41001, dtype)
