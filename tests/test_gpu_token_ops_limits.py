@@ -369,3 +369,132 @@ def test_gradients_into_and_past_the_caches(rows, vocab, dtype):
 def test_loss_of_rows_in_slices_and_whole(rows, dtype):
     """72 rows of 32 bits and 96 of 16 are the most that are cut into slices."""
     check_token_loss(rows, 41001, dtype)
+
+
+# the widest rows that a group's registers hold, and the first that they do not: pieces of 16 bytes of 8 (fp32: 4) logits
+@pytest.mark.parametrize("rows,vocab,dtype", [(97, 65536, "bf16"), (97, 65537, "fp16"), (97, 131071, "fp16"), (97, 131079, "bf16"), (97, 204799, "bf16"), (97, 204801, "fp16"), (97, 210001, "bf16"),
+                                              (97, 32767, "fp32"), (97, 32773, "fp32"), (97, 65535, "fp32"), (97, 65541, "fp32"), (97, 102400, "fp32"), (97, 102405, "fp32")])
+def test_loss_of_long_rows_that_are_whole(rows, vocab, dtype):
+    check_token_loss(rows, vocab, dtype)
+
+
+@pytest.mark.parametrize("vocab,dtype", [(180001, "bf16"), (210001, "bf16"), (90001, "fp32"), (120001, "fp32")])
+def test_long_whole_rows_that_are_not_numbers(vocab, dtype):
+    x = torch.randn(100, vocab, device="cuda", generator=rnd(1)).to(TYPES[dtype])
+    x[1, 7], x[2, vocab - 1] = math.nan, math.inf
+    x[3] = -math.inf
+    x[3, 5] = math.nan
+    x[4] = -math.inf
+    t, z = torch.zeros(100, dtype=torch.int32, device="cuda"), torch.zeros(100, device="cuda")
+    t[5] = vocab
+    x[5] = math.nan
+    for ent_coef in (0.0, 0.1):
+        d, stats, logp = L.token_loss(x, t, z, z + 1, ent_coef=ent_coef)
+        assert stats[7].item() == 1.0 and stats[6].item() == 98
+        bad = torch.zeros(100, dtype=torch.bool, device="cuda")
+        bad[1:4] = True
+        assert torch.equal(torch.isnan(d).any(1), bad) and torch.equal(torch.isnan(logp), bad) and not bool(d[4:6].any())
+
+
+@pytest.mark.parametrize("rows", [0, 1])
+@pytest.mark.parametrize("vocab", [1, 600, 50000, 1 << 24])
+def test_the_smallest_and_the_widest_rows(rows, vocab):
+    x = torch.randn(rows, vocab, device="cuda", generator=rnd(2))
+    t = torch.full((rows,), vocab - 1, dtype=torch.int32, device="cuda")
+    z = torch.zeros(rows, device="cuda")
+    logp, ent, stat = L.token_logp(x, t, want_entropy=True)
+    d, stats, again = L.token_loss(x, t, logp, z + 1, ent_coef=0.5)
+    back = L.token_logp_backward(x, t, stat, -(z + 1), entropy=ent, dentropy=z - 0.5)
+    assert stats[6].item() == rows and d.shape == back.shape == x.shape
+    if rows:
+        q = torch.log_softmax(x.double(), 1)
+        H = -(q.exp() * q).sum()
+        want = q.exp() * (1 + 0.5 * (q + H))
+        want[0, -1] -= 1
+        # sums of V terms in 64 V / V .. running sums: V / 64 + 32 roundings, of which the random ones cancel; the entropy's coefficient is off by
+        # as much of H = 17
+        tol = U32 * (vocab / 64 + 64)
+        assert abs(logp.item() - q[0, -1].item()) <= tol + 4 * U32 * 17 and abs(ent.item() - H.item()) <= 20 * tol
+        for got in (d, back):
+            assert bool(((got.double() - want).abs() <= q.exp() * 20 * tol + U32 * 64 * want.abs() + 1e-30).all())
+
+
+def test_the_most_rows():
+    rows = (1 << 24) - 1
+    x = torch.randn(rows, 2, device="cuda", generator=rnd(3))
+    t = torch.randint(-1, 2, (rows,), device="cuda", generator=rnd(4)).to(torch.int32)
+    z = torch.ones(rows, device="cuda")
+    active = t >= 0
+    want = torch.where(active, torch.nn.functional.logsigmoid(torch.where(t == 1, -1, 1) * (x[:, 0] - x[:, 1]).double()), 0.0)
+    logp, _, stat = L.token_logp(x, t)
+    assert float((logp.double() - want).abs().max()) <= U32 * 80
+    back = L.token_logp_backward(x, t, stat, z)
+    d, stats, again = L.token_loss(x, t, logp, -z)
+    p = torch.where(active, -torch.expm1(want), 0.0)   # 1 - p_t
+    grad = torch.stack([torch.where(t == 0, p, -p), torch.where(t == 1, p, -p)], 1)
+    assert float((back.double() - grad).abs().max()) <= U32 * 200 and float((d.double() - grad).abs().max()) <= U32 * 200
+    assert stats[6].item() == int(active.sum()) and abs(stats[0].item() / int(active.sum()) - 1) <= 1e-5
+    y = L.dropout(x, 0.5, 9)
+    part = torch.arange(rows - 1000, rows, device="cuda")
+    assert torch.equal(y[-1000:], L.dropout(x[-1000:], 0.5, 9, row_ids=part))
+
+
+def test_the_longest_dropout_row():
+    from test_gpu_token_ops import mask_definition
+    cols, q = 1 << 30, 32768
+    x = torch.ones(1, cols, dtype=torch.bfloat16, device="cuda")
+    y = L.dropout(x, 0.5, 7, out=x)
+    step = 1 << 22   # 2^22 columns at every one of 7 places, by the definition
+    import numpy as np
+    for at in (0, 1 << 28, (1 << 29) - step // 2, 1 << 29, 3 << 28, cols - step):
+        with np.errstate(over="ignore"):
+            keep = _mask_of_columns(7, 0, 0, at, step, q)
+        assert np.array_equal((y[0, at:at + step] != 0).cpu().numpy(), keep), at
+    assert np.array_equal((y[:, :4096] != 0).cpu().numpy(), mask_definition(7, 0, [0], 4096, q))
+
+
+def _mask_of_columns(seed, layer, row, first, n, border):
+    """mask_definition for the columns from `first` on (a multiple of 4)."""
+    import numpy as np
+    u, G = np.uint64, 0x9E3779B97F4A7C15
+
+    def mix(z):
+        z = (z ^ (z >> u(30))) * u(0xBF58476D1CE4E5B9)
+        z = (z ^ (z >> u(27))) * u(0x94D049BB133111EB)
+        return z ^ (z >> u(31))
+
+    s = mix(np.array([(seed + G) % (1 << 64)], np.uint64))
+    s = mix(s ^ u((layer + G) % (1 << 64)))
+    s = mix(s ^ u((row + G) % (1 << 64)))
+    c = first + np.arange(n)
+    z = mix(s[0] + (c // 4 + 1).astype(np.uint64) * u(G))
+    return ((z >> (c % 4 * 16).astype(np.uint64)) & u(0xFFFF)) >= u(border)
+
+
+def test_the_most_pairs():
+    """2^23 - 1 pairs of one token each: every margin by itself, the statistics over all."""
+    pairs = (1 << 23) - 1
+    logp = -torch.rand(2 * pairs, device="cuda", generator=rnd(5))
+    off = torch.arange(2 * pairs + 1, device="cuda")
+    grad, margin, stats = L.pair_loss(logp, off, beta=0.5, scale=1.0 / pairs)
+    D = 0.5 * (logp[:pairs].double() - logp[pairs:].double())
+    assert bool(((margin.double() - D).abs() <= 2 * U32 * D.abs()).all())
+    slope = -0.5 * torch.sigmoid(-D) / pairs
+    assert bool(((grad[:pairs].double() - slope).abs() <= 4 * U32 * slope.abs()).all()) and torch.equal(grad[pairs:], -grad[:pairs])
+    loss = torch.nn.functional.softplus(-D).sum().item() / pairs
+    assert abs(stats[0].item() - loss) <= 4 * U32 * loss and stats[5].item() == pairs and abs(stats[1].item() - (D > 0).double().mean().item()) <= 2 * U32
+
+
+def test_many_empty_sequences():
+    """More empty sequences than tokens, in front of, between and behind those that have some."""
+    T, n = 5000, 300000
+    cut = torch.randint(0, T + 1, (n - 1,), device="cuda", generator=rnd(6)).sort()[0]
+    cut[cut < 60] = 0
+    cut[(cut > 2000) & (cut < 4000)] = 2000
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), cut, torch.full((1,), T, device="cuda")])
+    r, v, last = torch.randn(T, device="cuda"), torch.randn(T, device="cuda"), torch.randn(n, device="cuda")
+    adv, ret = L.token_gae(r, v, off, 0.99, 0.95, last_value=last)
+    full = torch.nonzero(off[1:] > off[:-1])[:, 0]
+    few = torch.cat([off[full], off[-1:]])
+    again = L.token_gae(r, v, few, 0.99, 0.95, last_value=last[full])
+    assert torch.equal(adv, again[0]) and torch.equal(ret, again[1])
