@@ -241,7 +241,8 @@ def permutation_static(S: int, seed: int, update_idx: int, epoch: int, out=None,
 
 # ---- operators of a policy that answers in tokens (include/ppo_learner.h has the formulas).  They take CUDA tensors and allocate
 # their results with torch; a matrix may have any row stride.  Work runs on the device of the tensors, on `stream`: None is torch's
-# current stream of that device, and with another one the results belong to it (inputs must be ready on it, as with any stream).
+# current stream of that device, and with another one the results belong to it (inputs must be ready on it, as with any stream; they may be
+# dropped at once).
 # They stand outside autograd: inputs that require a gradient are taken as they are, results carry no history (a gradient of the logits goes
 # on with logits.backward(dlogits)), and `out` counts as a change in place of its tensor.
 
@@ -255,6 +256,9 @@ def _on_stream(first, stream, call, *args):
             raise ValueError(f"the tensors are on {first.device}, the stream on {stream.device}")
         with torch.cuda.stream(stream):
             out = call(stream.cuda_stream, *args)
+        for t in args:   # an input may be dropped by the caller as soon as this returns: its memory is not given away before the work is done
+            if isinstance(t, torch.Tensor):
+                t.record_stream(stream)
     if out[0]:
         raise LearnerError(out[0], _lib.ppo_last_error(None).decode())
     return out

@@ -498,3 +498,41 @@ def test_many_empty_sequences():
     few = torch.cat([off[full], off[-1:]])
     again = L.token_gae(r, v, few, 0.99, 0.95, last_value=last[full])
     assert torch.equal(adv, again[0]) and torch.equal(ret, again[1])
+
+
+def test_inputs_dropped_while_another_stream_reads_them():
+    """Inputs that the caller drops behind a call on another stream keep their memory until that stream has read them."""
+    side, n = torch.cuda.Stream(), 1 << 22
+    ids, t = torch.arange(n // 64, device="cuda"), torch.zeros(n // 64, dtype=torch.int32, device="cuda")
+    calls = (lambda x, s: L.dropout(x, 0.5, 3, row_ids=ids, stream=s), lambda x, s: L.token_logp(x, t, stream=s)[0],
+             lambda x, s: L.token_gae(x.view(-1), x.view(-1), ids * 64, 0.9, 0.9, stream=s)[0])
+    for call in calls:
+        torch.cuda.empty_cache()
+        x = torch.randn(n // 64, 64, device="cuda", generator=rnd(1))
+        want, place = call(x.clone(), None), x.data_ptr()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(100_000_000)   # the call waits behind this
+        got = call(x, side)
+        del x
+        other = [torch.full((n // 64, 64), math.nan, device="cuda") for _ in range(4)]
+        assert all(o.data_ptr() != place for o in other)
+        side.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_a_recording_on_the_stream_that_is_given():
+    """stream= inside a recording on that stream, replayed with new inputs."""
+    x, t = torch.randn(300, 700, device="cuda"), torch.randint(0, 700, (300,), device="cuda").to(torch.int32)
+    z, side, graph = torch.zeros(300, device="cuda"), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    L.token_loss(x, t, z, z + 1)
+    torch.cuda.synchronize()
+    old, adv = z - 6, z + 1
+    with torch.cuda.graph(graph, stream=side):
+        out = L.token_loss(x, t, old, adv, ent_coef=0.1, stream=side)
+    for turn in range(3):
+        x.copy_(torch.randn(300, 700, device="cuda", generator=rnd(turn)))
+        graph.replay()
+        want = L.token_loss(x, t, old, adv, ent_coef=0.1)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, want)), turn
