@@ -290,7 +290,8 @@ int ppo_token_logp_backward(int32_t dtype, int64_t rows, int64_t vocab, const vo
  * its gradient, in one pass over the logits.  With rho = exp(logp - logp_old) and x = logp_ref - logp, a token's loss is
  *   l = -min(rho A, clip(rho, 1 - clip_lo, 1 + clip_hi) A) + kl_coef (exp x - x - 1) - ent_coef H
  * (exp x - x - 1: the non-negative one-sample estimate of KL(policy || reference)), and L = scale sum_r weight_r l_r over
- * the rows that are not idle.  At ties the unclipped branch carries the gradient. */
+ * the rows that are not idle.  At ties the unclipped branch carries the gradient.  A weight of 0 hides no term that is infinite or no
+ * number: rows that do not count (padding) have a target outside [0, vocab). */
 typedef struct {
   float temperature;      /* > 0, and large enough for 2 / temperature to be finite */
   float clip_lo, clip_hi; /* >= 0; clip_lo <= 1 */
@@ -309,7 +310,7 @@ int ppo_token_loss(int32_t dtype, int64_t rows, int64_t vocab, const void* d_log
                    int64_t ws_bytes, void* hip_stream);
 
 /* Sequences of the calls below are packed one behind the other: sequence k holds the tokens [d_offsets[k], d_offsets[k+1])
- * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty; tokens <= 2^34).  Offsets outside [0, tokens] are taken as its
+ * (int64, non-decreasing, inside [0, tokens]; a sequence may be empty; tokens <= 2^34, sequences <= 2^30).  Offsets outside [0, tokens] are taken as its
  * nearer end, and of decreasing ones the results are unspecified; no memory outside the arrays is touched either way.
  * d_mask: uint8 [tokens], 0 = the token is passed over (a prompt, a tool's answer) and its inputs may be anything; NULL: none.
  * (Tokens whose row was idle in ppo_token_logp, with a log-probability of 0, belong there.)

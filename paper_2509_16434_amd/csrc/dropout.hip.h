@@ -5,8 +5,10 @@
 // So y = keep ? x * 65536 / (65536 - q) : 0, plus the residual, in fp32, rounded once to the tensors' type.  The backward
 // pass is the same call on the gradient.
 //
-// Bound by memory: an output serves four columns (fp32) or two outputs eight (16 bits), about 15 vector instructions a column
-// where the time of its bytes holds 35; the hash of (seed, layer) is made on the host, that of the row id once per thread.
+// Bound by memory: an output serves four columns (fp32) or two outputs eight (16 bits), 13 vector instructions a column (16 with the
+// residual) where the time of its bytes holds 22 (38); the hash of (seed, layer) is made on the host, that of the row id once per thread.
+// Pieces are cut from the row's start, where the generator's outputs begin: rows of odd length cross the boundaries of cache lines and run at
+// 0.94 of the rate (134 MB each way in the last-level cache: 16384 x 4096 bf16 7030 GB/s, 16388 x 4095 6600).
 #pragma once
 #include "elem.hip.h"
 #include "splitmix.hip.h"

@@ -15,7 +15,7 @@
 //
 // Measured (GB/s of one read and, for gradients, one write of every logit; a plain copy of 2 GiB reaches 4490, reading alone 5200):
 //   log-probability   8192 x 50257 fp16 5790, 8192 x 131072 bf16 6040, 65536 x 1000 bf16 5100
-//   loss              16384 x 131072 bf16 5480, 8192 x 32000 bf16 5090, 3001 x 50257 bf16 with entropy 4900, 32768 x 2000 bf16 4950, 131072 x 257 bf16 3560
+//   loss              16384 x 131072 bf16 5480, 8192 x 32000 bf16 5090, 3001 x 50257 bf16 with entropy 4900, 32768 x 2000 bf16 with entropy 4700, 131072 x 257 bf16 with entropy 3460
 //   backward          4096 x 32000 fp32 5800
 #pragma once
 #include "elem.hip.h"
@@ -348,8 +348,8 @@ __device__ __forceinline__ LossRecord loss_idle(const RowArgs& a, int64_t row, T
 }
 
 // Loss and gradient of rows of at most G K pieces by groups of G threads: the row stays in registers (as it is, 16 bits packed) between
-// the passes that find the maximum, add up and write, so that memory sees it once in and once out.  Exponentials are made twice; 18 to 22
-// vector instructions a logit of 16 bits keep the vector units busy for 0.6 of the time of its bytes (16384 x 131072).
+// the passes that find the maximum, add up and write, so that memory sees it once in and once out.  Exponentials are made twice; 15
+// vector instructions a logit of 16 bits, 21 with the entropy, keep the vector units busy for 0.65 of the time (16384 x 131072; 3001 x 50257).
 template <class T, int G, int K, bool ENT>
 __device__ __forceinline__ LossRecord loss_in_registers(const RowArgs& a, int64_t row, int tid, float* lds) {
   constexpr int N = Piece<T>::N;

@@ -239,7 +239,10 @@ __global__ __launch_bounds__(1024) void k_pair_stats_join(int blocks, float scal
 // Bound: 16 to 17 bytes a token, the inputs twice (from the last-level cache the second time) where there is more than one tile:
 // 3 M tokens 9.8 + 14.6 us, 11 at the rate of a copy; 200000 tokens 5.2 + 6.4 us, which is latency.
 constexpr int GAE_PER = 8, GAE_TILE = 256 * GAE_PER;   // tokens per thread and per tile
-constexpr int GAE_DIRECT = 4096;                       // at most so many tiles are scanned directly
+// At most so many tiles (8.4 M tokens) are scanned directly.  What that costs goes by how far the ends of sequences lie apart, which the host does
+// not know: us a call directly and with k_gae_tiles, one sequence: 3 M tokens 26 and 32, 6 M 57 and 54, 8.3 M 85 and 68, 16 M 222 and 120,
+// 33 M 774 and 253; 24 sequences: 3 M 23 and 32, 8.3 M 50 and 68, 16 M 84 and 120, 33 M 198 and 253.
+constexpr int GAE_DIRECT = 4096;
 struct GaeMap { double a, b, c; float v; int32_t set, stop, offset; };   // set: V -> v, else V stays; stop: nothing from behind
                                                                        // matters; offset: first_above at the tile's start
 struct GaeArgs {
