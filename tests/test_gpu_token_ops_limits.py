@@ -536,3 +536,59 @@ def test_a_recording_on_the_stream_that_is_given():
         want = L.token_loss(x, t, old, adv, ent_coef=0.1)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), turn
+
+
+def test_what_is_not_a_number_stays_in_its_sequence():
+    """NaN and infinities among a sequence's tokens reach its earlier tokens and nothing else, within a tile and across tiles."""
+    lengths = [5, 3000, 1, 0, 7000, 2, 4100]
+    off = torch.tensor([0] + lengths, device="cuda").cumsum(0)
+    T = int(off[-1])
+    r, v, last = torch.randn(T, generator=rnd(1), device="cuda"), torch.randn(T, generator=rnd(2), device="cuda"), torch.randn(len(lengths), generator=rnd(3), device="cuda")
+    clean = L.token_gae(r, v, off, 0.99, 0.95, last_value=last)
+    for seq, at, place, value in ((1, 2500, r, math.nan), (4, 6000, v, math.inf), (4, 0, r, -math.inf), (6, 4099, v, math.nan), (5, None, last, math.nan), (0, 4, r, math.inf)):
+        a, b, c = r.clone(), v.clone(), last.clone()
+        (a if place is r else b if place is v else c)[seq if place is last else int(off[seq]) + at] = value
+        adv, ret = L.token_gae(a, b, off, 0.99, 0.95, last_value=c)
+        end = int(off[seq + 1]) if at is None else int(off[seq]) + at + 1
+        bad = torch.zeros(T, dtype=torch.bool, device="cuda")
+        bad[int(off[seq]):end] = True
+        assert torch.equal(~torch.isfinite(adv), bad)
+        assert all(torch.equal(x[~bad], y[~bad]) for x, y in zip((adv, ret), clean))
+    # pairs: the other pairs' gradients and margins stay
+    off = torch.tensor([0, 5, 3005, 3006, 10006, 10008, 14108], device="cuda")
+    clean = L.pair_loss(r[:14108], off)
+    x = r[:14108].clone()
+    x[3005] = math.nan   # the third chosen one's
+    grad, margin, stats = L.pair_loss(x, off)
+    bad = torch.zeros(14108, dtype=torch.bool, device="cuda")
+    bad[3005:3006], bad[10008:] = True, True
+    assert torch.equal(torch.isnan(grad), bad) and torch.equal(grad[~bad], clean[0][~bad]) and torch.equal(margin[:2], clean[1][:2]) and stats[6].item() == 1
+
+
+def test_tokens_beyond_32_bits():
+    """2^32 tokens and some, in sequences that cross 2^31 and 2^32: constant rewards give geometric sums, constant log-probabilities known ones."""
+    T, gl = (1 << 32) + 12293, 0.96875 * 0.5
+    bounds = [0, 7, (1 << 31) - 5000, (1 << 31) + 3, (1 << 32) - 3, (1 << 32) + 5000, T]
+    off = torch.tensor(bounds, device="cuda")
+    r = torch.ones(T, device="cuda")
+    v = torch.zeros(T, device="cuda")
+    adv, ret = L.token_gae(r, v, off, 0.96875, 0.5)
+    for lo, hi in zip(bounds, bounds[1:]):
+        for at in (lo, lo + 1, (lo + hi) // 2, hi - 3, hi - 2, hi - 1):
+            want = (1 - gl ** (hi - at)) / (1 - gl)
+            assert abs(adv[at].item() - want) <= 2 * U32 * want and ret[at].item() == adv[at].item(), at
+    assert float(adv.amin()) >= 1 and float(adv.amax()) < 1 / (1 - gl) * (1 + 2 * U32)
+    del v, ret
+    # 0.5 each: differences of the sequences' lengths, halved; exact in 64 bits
+    r.fill_(0.5)
+    grad, margin, stats = L.pair_loss(r, off, kind="squared", beta=0.5)
+    n = [b - a for a, b in zip(bounds, bounds[1:])]
+    for k in range(3):
+        D = 0.5 * (n[k] - n[k + 3])
+        assert abs(margin[k].item() - 0.5 * D) <= 2 * U32 * abs(0.5 * D)
+        slope = 2 * (D - 1)
+        for s, sign in ((k, 1), (k + 3, -1)):
+            for at in (bounds[s], bounds[s + 1] - 1, (bounds[s] + bounds[s + 1]) // 2):
+                assert abs(grad[at].item() - sign * slope) <= 2 * U32 * abs(slope)
+    del r, adv, grad
+    torch.cuda.empty_cache()
